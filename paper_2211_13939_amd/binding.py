@@ -49,6 +49,9 @@ EXPORTS = (
     "tts_encoder_destroy",
 )
 
+# every symbol include/tts_norm.h, tts_linear8.h and tts_cross.h declare
+OPERATOR_EXPORTS = tuple(f"tts_{op}_{call}" for op in ("norm", "linear8", "cross") for call in ("workspace_bytes", "create", "run", "destroy"))
+
 _fp = C.POINTER(C.c_float)
 _ip = C.POINTER(C.c_int)
 _i64p = C.POINTER(C.c_int64)
@@ -86,6 +89,34 @@ class TtsEncoderConfig(C.Structure):
 
 class TtsEncoderWeights(C.Structure):
     _fields_ = [("tables", _fp * 4), ("conv_w", _fp * 3), ("conv_b", _fp * 3), ("w_ih", _fp * 2), ("w_hh", _fp * 2), ("b", _fp * 2)]
+
+
+class TtsNormConfig(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("dim", "kind", "x_dtype", "res_dtype", "y_dtype")] + [("eps", C.c_float)]
+
+
+class TtsNormRows(C.Structure):
+    _fields_ = [("rows", C.c_int), ("x", C.c_void_p), ("x_stride", C.c_longlong), ("res", C.c_void_p), ("res_stride", C.c_longlong),
+                ("total", C.c_void_p), ("total_stride", C.c_longlong), ("y", C.c_void_p), ("y_stride", C.c_longlong),
+                ("y8", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class TtsLinear8Config(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("in_dim", "out_dim", "y_dtype")]
+
+
+class TtsCrossConfig(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("n_heads", "n_kv_heads", "head_dim", "dtype")]
+
+
+class TtsCrossBatch(C.Structure):
+    _fields_ = [("n", C.c_int), ("q_len", _ip), ("mem_row", C.POINTER(C.c_longlong)), ("mem_len", _ip)]
+
+
+class TtsCrossTensors(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_longlong), ("k", C.c_void_p), ("k_stride", C.c_longlong),
+                ("v", C.c_void_p), ("v_stride", C.c_longlong), ("out", C.c_void_p), ("out_stride", C.c_longlong),
+                ("keep", C.c_void_p), ("lse", C.c_void_p), ("scale", C.c_float)]
 
 
 VOCODER_HOP = 256
@@ -182,6 +213,21 @@ def lib() -> C.CDLL:
     L.tts_encoder_elapsed_ms.argtypes = [vp, _fp]
     L.tts_encoder_destroy.restype = None
     L.tts_encoder_destroy.argtypes = [vp]
+    L.tts_norm_workspace_bytes.restype = C.c_size_t
+    L.tts_norm_workspace_bytes.argtypes = [C.POINTER(TtsNormConfig)]
+    L.tts_norm_create.argtypes = [C.POINTER(TtsNormConfig), _fp, vp, C.c_size_t, vp, C.POINTER(vp)]
+    L.tts_norm_run.argtypes = [vp, C.POINTER(TtsNormRows)]
+    L.tts_linear8_workspace_bytes.restype = C.c_size_t
+    L.tts_linear8_workspace_bytes.argtypes = [C.POINTER(TtsLinear8Config)]
+    L.tts_linear8_create.argtypes = [C.POINTER(TtsLinear8Config), _fp, _fp, vp, C.c_size_t, vp, C.POINTER(vp)]
+    L.tts_linear8_run.argtypes = [vp, vp, vp, C.c_int, vp, C.c_longlong]
+    L.tts_cross_workspace_bytes.restype = C.c_size_t
+    L.tts_cross_workspace_bytes.argtypes = [C.POINTER(TtsCrossConfig)]
+    L.tts_cross_create.argtypes = [C.POINTER(TtsCrossConfig), vp, C.c_size_t, vp, C.POINTER(vp)]
+    L.tts_cross_run.argtypes = [vp, C.POINTER(TtsCrossBatch), C.POINTER(TtsCrossTensors)]
+    for f in (L.tts_norm_destroy, L.tts_linear8_destroy, L.tts_cross_destroy):
+        f.restype = None
+        f.argtypes = [vp]
     _lib = L
     return L
 
@@ -745,3 +791,202 @@ class Encoder:
             self.close()
         except Exception:
             pass
+
+
+SCALE_BLOCK = 128         # columns of an 8-bit row under one scale
+NORM_RMS, NORM_NONE = 0, 1
+
+
+def width8(dim: int) -> int:
+    """Columns of an 8-bit row: whole blocks of 128."""
+    return -(-dim // SCALE_BLOCK) * SCALE_BLOCK
+
+
+def scale_columns(dim: int) -> int:
+    """Scales of an 8-bit row: whole words of four."""
+    return -(-width8(dim) // (4 * SCALE_BLOCK)) * 4
+
+
+class _Operator:
+    """An object on a stream with an arena of its own, as the modules above have them."""
+
+    _name = ""
+
+    def _setup(self, cfg, stream, device):
+        import torch
+        if not torch.cuda.is_available():
+            raise RuntimeError(f"no GPU visible: tts_{self._name} has no CPU path")
+        self._torch = torch
+        self.cfg = cfg
+        d = torch.device(device)
+        self.device = torch.device(d.type, torch.cuda.current_device() if d.index is None else d.index)
+        nbytes = int(getattr(lib(), f"tts_{self._name}_workspace_bytes")(C.byref(cfg)))
+        if nbytes == 0:
+            raise TtsError(TTS_E_INVAL, lib().tts_last_error().decode("utf-8", "replace"))
+        with torch.cuda.device(self.device):
+            self.arena = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self.stream = stream if stream is not None else torch.cuda.Stream(device=self.device)
+            torch.cuda.current_stream().synchronize()      # (the arena's memory may have been in use on this stream)
+        self._handle = C.c_void_p()
+        self._run = getattr(lib(), f"tts_{self._name}_run")
+        return C.c_void_p(self.arena.data_ptr()), nbytes, C.c_void_p(self.stream.cuda_stream), C.byref(self._handle)
+
+    def _type(self, dtype: int):
+        return self._torch.bfloat16 if dtype == DTYPE_BF16 else self._torch.float32
+
+    def _at(self, t, name, dtype, shape) -> int:
+        """Address of a tensor of this device, type and shape whose elements lie back to back."""
+        self._like(t, name, dtype, shape)
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: its elements have to lie back to back")
+        return t.data_ptr()
+
+    def _rows(self, t, name, dtype, shape):
+        """(address, distance of the rows) of one whose rows may lie apart; 0: back to back."""
+        self._like(t, name, dtype, shape)
+        if t.is_contiguous():
+            return t.data_ptr(), 0
+        if t.stride(0) <= 0 or not t[0].is_contiguous():
+            raise ValueError(f"{name}: the elements of a row have to lie back to back")
+        return t.data_ptr(), t.stride(0)
+
+    def _like(self, t, name, dtype, shape) -> None:
+        if t.device != self.device or t.dtype != dtype or t.shape != shape:
+            raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device} where {tuple(shape)} {dtype} on {self.device} is wanted")
+
+    def close(self) -> None:
+        if getattr(self, "_handle", None):
+            getattr(lib(), f"tts_{self._name}_destroy")(self._handle)
+            self._handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def make_norm_config(dim: int, x_bf16: bool = False, res_bf16: bool = False, y_bf16: bool = False, eps: float = 1e-5,
+                     kind: int = NORM_RMS) -> TtsNormConfig:
+    pick = lambda b: DTYPE_BF16 if b else DTYPE_F32   # noqa: E731
+    return TtsNormConfig(int(dim), int(kind), pick(x_bf16), pick(res_bf16), pick(y_bf16), float(eps))
+
+
+class Norm(_Operator):
+    """tts_norm_* calls: residual's addition, root-mean-square norm (kind NORM_NONE: none) and output in 8 bits with scales."""
+
+    _name = "norm"
+
+    def __init__(self, cfg: TtsNormConfig, gain=None, stream=None, device: str = "cuda:0"):
+        where = self._setup(cfg, stream, device)
+        g = None if gain is None else np.ascontiguousarray(gain, np.float32)
+        if g is not None and g.shape != (cfg.dim,):
+            raise ValueError(f"gain: {g.shape} where ({cfg.dim},) is wanted")
+        _check(lib().tts_norm_create(C.byref(cfg), None if g is None else g.ctypes.data_as(_fp), *where))
+        self._types = [self._type(t) for t in (cfg.x_dtype, cfg.res_dtype, cfg.res_dtype, cfg.y_dtype)]
+
+    def run_device(self, x, res=None, total=None, y=None, y8=None, scales=None) -> None:
+        """x, res, total, y: CUDA [rows, dim] of the configuration's types, rows any distance apart; y8: float8_e4m3fn [rows, width8(dim)],
+        scales: float8_e8m0fnu [rows, scale_columns(dim)].  Those that are None are not there.  Queued on the stream."""
+        shape, t = x.shape, self._types
+        if len(shape) != 2 or shape[1] != self.cfg.dim:
+            raise ValueError(f"x: {tuple(shape)} where [rows, {self.cfg.dim}] is wanted")
+        a = TtsNormRows()
+        a.rows = shape[0]
+        a.x, a.x_stride = self._rows(x, "x", t[0], shape)
+        if res is not None:
+            a.res, a.res_stride = self._rows(res, "res", t[1], shape)
+        if total is not None:
+            a.total, a.total_stride = self._rows(total, "total", t[2], shape)
+        if y is not None:
+            a.y, a.y_stride = self._rows(y, "y", t[3], shape)
+        if y8 is not None:
+            a.y8 = self._at(y8, "y8", self._torch.float8_e4m3fn, (shape[0], width8(shape[1])))
+        if scales is not None:
+            a.scales = self._at(scales, "scales", self._torch.float8_e8m0fnu, (shape[0], scale_columns(shape[1])))
+        rc = self._run(self._handle, C.byref(a))
+        if rc:
+            _check(rc)
+
+
+def make_linear8_config(in_dim: int, out_dim: int, bf16: bool = False) -> TtsLinear8Config:
+    return TtsLinear8Config(int(in_dim), int(out_dim), DTYPE_BF16 if bf16 else DTYPE_F32)
+
+
+class Linear8(_Operator):
+    """tts_linear8_* calls: the product of 8-bit rows with 8-bit weights, a scale for each 128 columns.  w: fp32 [out_dim, in_dim] (host)."""
+
+    _name = "linear8"
+
+    def __init__(self, cfg: TtsLinear8Config, w, bias=None, stream=None, device: str = "cuda:0"):
+        where = self._setup(cfg, stream, device)
+        w = np.ascontiguousarray(w, np.float32)
+        b = None if bias is None else np.ascontiguousarray(bias, np.float32)
+        if w.shape != (cfg.out_dim, cfg.in_dim) or (b is not None and b.shape != (cfg.out_dim,)):
+            raise ValueError(f"w: {w.shape}, bias: {None if b is None else b.shape} where {(cfg.out_dim, cfg.in_dim)} and {(cfg.out_dim,)} are wanted")
+        _check(lib().tts_linear8_create(C.byref(cfg), w.ctypes.data_as(_fp), None if b is None else b.ctypes.data_as(_fp), *where))
+        self._y_type = self._type(cfg.y_dtype)
+
+    def run_device(self, x8, scales, y) -> None:
+        """x8: CUDA float8_e4m3fn [rows, width8(in_dim)], zeros past in_dim; scales: float8_e8m0fnu [rows, scale_columns(in_dim)]; y: [rows, out_dim],
+        rows any distance apart.  Queued on the stream."""
+        rows, k = x8.shape[0], self.cfg.in_dim
+        at = self._at(x8, "x8", self._torch.float8_e4m3fn, (rows, width8(k)))
+        sx = self._at(scales, "scales", self._torch.float8_e8m0fnu, (rows, scale_columns(k)))
+        rc = self._run(self._handle, at, sx, rows, *self._rows(y, "y", self._y_type, (rows, self.cfg.out_dim)))
+        if rc:
+            _check(rc)
+
+
+def make_cross_config(n_heads: int, n_kv_heads: int, head_dim: int, bf16: bool = False) -> TtsCrossConfig:
+    return TtsCrossConfig(int(n_heads), int(n_kv_heads), int(head_dim), DTYPE_BF16 if bf16 else DTYPE_F32)
+
+
+class CrossBatch:
+    """The lengths of a dynamic batch: queries, first memory row and memory rows of every request."""
+
+    def __init__(self, q_len, mem_row, mem_len):
+        n = len(q_len)
+        if len(mem_row) != n or len(mem_len) != n:
+            raise ValueError("q_len, mem_row and mem_len have a value for each request")
+        self._keep = ((C.c_int * n)(*map(int, q_len)), (C.c_longlong * n)(*map(int, mem_row)), (C.c_int * n)(*map(int, mem_len)))
+        self.queries = sum(self._keep[0])
+        self.memory_rows = max((r + m for r, m in zip(self._keep[1], self._keep[2]) if m > 0), default=0)      # that k and v have to have
+        self.c = TtsCrossBatch(n, *self._keep)
+
+
+class CrossAttention(_Operator):
+    """tts_cross_* calls: attention of a dynamic batch's queries to its requests' memories."""
+
+    _name = "cross"
+
+    def __init__(self, cfg: TtsCrossConfig, stream=None, device: str = "cuda:0"):
+        where = self._setup(cfg, stream, device)
+        _check(lib().tts_cross_create(C.byref(cfg), *where))
+        self._dtype = self._type(cfg.dtype)
+
+    def batch(self, q_len, mem_row, mem_len) -> CrossBatch:
+        """A batch's lengths, for any number of calls."""
+        return CrossBatch(q_len, mem_row, mem_len)
+
+    def run_device(self, batch: CrossBatch, q, k, v, out, keep=None, lse=None, scale: float = 0.0) -> None:
+        """q, out: CUDA [queries, n_heads, head_dim]; k, v: [memory rows, n_kv_heads, head_dim], rows any multiple of 8 elements apart; keep: uint8
+        [memory rows], 0 = hidden; lse: fp32 [queries, n_heads].  Queued on the stream; scale 0: 1 / sqrt(head_dim)."""
+        c, t = self.cfg, self._dtype
+        rows = k.shape[0]
+        of_q, of_k = (batch.queries, c.n_heads, c.head_dim), (rows, c.n_kv_heads, c.head_dim)
+        if rows < batch.memory_rows:
+            raise ValueError(f"k has {rows} rows, the batch's memories end at {batch.memory_rows}")
+        a = TtsCrossTensors()
+        a.q, a.q_stride = self._rows(q, "q", t, of_q)
+        a.k, a.k_stride = self._rows(k, "k", t, of_k)
+        a.v, a.v_stride = self._rows(v, "v", t, of_k)
+        a.out, a.out_stride = self._rows(out, "out", t, of_q)
+        if keep is not None:
+            a.keep = self._at(keep, "keep", self._torch.uint8, (rows,))
+        if lse is not None:
+            a.lse = self._at(lse, "lse", self._torch.float32, of_q[:2])
+        a.scale = scale
+        rc = self._run(self._handle, C.byref(batch.c), C.byref(a))
+        if rc:
+            _check(rc)

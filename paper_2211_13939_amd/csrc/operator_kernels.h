@@ -1,0 +1,54 @@
+// Host-visible launch wrappers of the operators' kernels (norm.hip, linear8.hip, cross.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace tts {
+
+constexpr int E8_BLOCK = 128;            // columns of an 8-bit row under one scale
+constexpr int width8(int dim) { return (dim + E8_BLOCK - 1) / E8_BLOCK * E8_BLOCK; }
+constexpr int scale_columns(int dim) { return (width8(dim) / E8_BLOCK + 3) / 4 * 4; }
+
+struct NormArgs {
+    const void *x, *res;                 // res: null if there is none
+    void *total, *y;                     // null: not wanted
+    uint8_t *y8, *scales;                // null: not wanted
+    const float* gain;                   // null: no norm
+    long long x_stride, res_stride, total_stride, y_stride;    // elements
+    int rows, dim;
+    float eps;
+    bool y_bf16;
+};
+hipError_t launch_norm(const NormArgs& a, bool x_bf16, bool res_bf16, int n_cu, hipStream_t s);
+
+struct Linear8Args {
+    const uint8_t *x8, *sx;              // [rows][width8], [rows][scale_columns]
+    const uint4* w;                      // [tiles of 16 channels][blocks][2 halves][64 lanes] 16 bytes: lane l holds channel l % 16, columns 64 * half + 16 * (l / 16) ..
+    const uint32_t* sw;                  // [tiles of 16 channels][words of scales][16 channels]
+    const float* bias;                   // [channels], zeros if there is none
+    void* y;
+    long long y_stride;
+    int rows, out_dim, blocks;           // blocks: of 128 columns
+};
+hipError_t launch_linear8(const Linear8Args& a, bool y_bf16, int n_cu, hipStream_t s);
+
+constexpr int CROSS_BATCH = 128;         // requests of a launch
+struct CrossReq {
+    long long mem_row;
+    int mem_len, q_row, q_len, pad;
+};
+struct CrossArgs {
+    const void *q, *k, *v;
+    void* out;
+    const uint8_t* keep;
+    float *lse, *parts;
+    long long q_stride, k_stride, v_stride, out_stride;        // elements
+    float scale;                         // times log2(e)
+    int n_heads, n_kv_heads, head_dim;
+    int n;
+    CrossReq req[CROSS_BATCH];
+};
+size_t cross_parts_bytes();
+hipError_t launch_cross(CrossArgs& a, bool bf16, int n_cu, hipStream_t s);
+
+}  // namespace tts

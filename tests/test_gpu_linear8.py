@@ -1,0 +1,151 @@
+"""tts_linear8 against its definition in 64 bits: sizes around the tiles' borders, both types of result, strides, scales from the least to the largest, graphs."""
+import numpy as np
+import pytest
+
+from paper_2211_13939_amd import binding
+from tests import operator_ref as ref
+from tests.helpers import say
+
+pytestmark = pytest.mark.gpu
+
+
+def _rows8(torch, v):
+    b, s = ref.round8(v.astype(np.float64))
+    return (b, s, torch.from_numpy(b).to("cuda:0").view(torch.float8_e4m3fn), torch.from_numpy(s).to("cuda:0").view(torch.float8_e8m0fnu))
+
+
+def _want(xb, xs, w, bias, bf16):
+    """The result in 64 bits, and how far a computed one may be off.
+    fp32: a sum of n terms in fp32 in any order is off by n half steps of the terms' sum of magnitudes; the bias's addition and the operand's
+    rounding (none) add one.  bf16: within a block, terms are aligned to the largest and lose less than 2^-16 of it each (the instruction's own
+    width); its 128 terms, over all blocks; then the result's rounding."""
+    wb, ws = ref.round8(w.astype(np.float64))
+    x, ww = ref.values8(xb, xs), ref.values8(wb, ws)
+    y = x @ ww.T + (0 if bias is None else bias.astype(np.float64))
+    size = np.abs(x) @ np.abs(ww).T + (0 if bias is None else np.abs(bias))
+    tol = (x.shape[1] + 16) * ref.EPS32 * size
+    if bf16:
+        rows, n = x.shape[0], w.shape[0]
+        for b in range(x.shape[1] // 128):
+            ax, aw = np.abs(x[:, b * 128:(b + 1) * 128]), np.abs(ww[:, b * 128:(b + 1) * 128])
+            tol += 128 * 2.0 ** -16 * np.minimum(ax.max(1)[:, None] * aw.max(1)[None, :], np.inf) * np.ones((rows, n))
+        tol += ref.EPS_BF16 * np.abs(y)
+    return y, tol
+
+
+@pytest.mark.parametrize("rows,k,n", [(1, 1, 1), (1, 1024, 512), (2, 127, 15), (15, 128, 16), (16, 129, 17), (17, 640, 250), (32, 1000, 64), (33, 2048, 48),
+                                      (64, 512, 1024), (65, 384, 130), (128, 256, 256), (129, 1024, 257), (200, 1500, 511), (256, 128, 512), (257, 300, 1000), (777, 1000, 1111)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_product_against_64_bits(rows, k, n, bf16):
+    import torch
+    say(f"case linear8 {rows} x {k} x {n} {'bf16' if bf16 else 'fp32'}")
+    rng = np.random.default_rng(rows + k + n)
+    x = rng.standard_normal((rows, k)) * np.exp(rng.standard_normal((rows, 1)))
+    w = (rng.standard_normal((n, k)) / np.sqrt(k)).astype(np.float32)
+    bias = rng.standard_normal(n).astype(np.float32) if (rows + n) % 2 else None
+    xb, xs, x8, sx = _rows8(torch, x)
+    op = binding.Linear8(binding.make_linear8_config(k, n, bf16), w, bias, stream=torch.cuda.current_stream())
+    pad = 3
+    whole = torch.full((rows + 2, n + pad), 9.0, dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda:0")
+    y = whole[1:-1, 1:n + 1]
+    op.run_device(x8, sx, y)
+    dense = torch.empty(rows, n, dtype=whole.dtype, device="cuda:0")
+    op.run_device(x8, sx, dense)
+    torch.cuda.synchronize()
+    want, tol = _want(xb, xs, w, bias, bf16)
+    assert (np.abs(y.double().cpu().numpy() - want) <= tol).all()
+    assert torch.equal(y, dense)
+    whole[1:-1, 1:n + 1] = 9.0
+    assert (whole == 9.0).all()                         # nothing around the rows was written
+    op.close()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_rows_do_not_depend_on_their_batch(bf16):
+    """What a row's neighbours are does not change it, within a form; across forms it stays within the tolerance."""
+    import torch
+    rng = np.random.default_rng(2)
+    w = rng.standard_normal((300, 700)).astype(np.float32)
+    xb, xs, x8, sx = _rows8(torch, rng.standard_normal((600, 700)))
+    op = binding.Linear8(binding.make_linear8_config(700, 300, bf16), w, stream=torch.cuda.current_stream())
+    want, tol = _want(xb, xs, w, None, bf16)
+    for rows in (1, 3, 16, 40, 64, 100, 256, 600):
+        y = torch.empty(rows, 300, dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda:0")
+        again = torch.empty_like(y)
+        op.run_device(x8[:rows], sx[:rows], y)
+        op.run_device(x8[:rows], sx[:rows], again)
+        torch.cuda.synchronize()
+        assert torch.equal(y, again)
+        assert (np.abs(y.double().cpu().numpy() - want[:rows]) <= tol[:rows]).all(), rows
+    op.close()
+
+
+@pytest.mark.parametrize("rows", [3, 300])
+def test_scales_from_small_to_large_and_zero_blocks(rows):
+    import torch
+    rng = np.random.default_rng(8)
+    k, n = 640, 40
+    x = rng.standard_normal((rows, k))
+    x[:, 128:256] *= 2.0 ** 40
+    x[:, 256:384] *= 2.0 ** -60
+    x[:, 384:512] = 0
+    w = rng.standard_normal((n, k)).astype(np.float32)
+    w[:, :128] *= 2.0 ** 20
+    w[:, 128:256] *= 2.0 ** -20
+    w[5] = 0
+    w[:, 512:640] = 0
+    xb, xs, x8, sx = _rows8(torch, x)
+    for bf16 in (False, True):
+        op = binding.Linear8(binding.make_linear8_config(k, n, bf16), w, stream=torch.cuda.current_stream())
+        y = torch.empty(rows, n, dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda:0")
+        op.run_device(x8, sx, y)
+        torch.cuda.synchronize()
+        want, tol = _want(xb, xs, w, None, bf16)
+        assert (np.abs(y.double().cpu().numpy() - want) <= tol).all()
+        assert (y[:, 5] == 0).all()
+        op.close()
+
+
+@pytest.mark.parametrize("rows", [1, 300])
+def test_a_nan_stays_in_its_row(rows):
+    import torch
+    rng = np.random.default_rng(1)
+    w = rng.standard_normal((70, 256)).astype(np.float32)
+    xb, xs, x8, sx = _rows8(torch, rng.standard_normal((rows, 256)))
+    x8.view(torch.uint8)[rows // 2, 77] = 0x7F
+    for bf16 in (False, True):
+        op = binding.Linear8(binding.make_linear8_config(256, 70, bf16), w, stream=torch.cuda.current_stream())
+        y = torch.empty(rows, 70, dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda:0")
+        op.run_device(x8, sx, y)
+        torch.cuda.synchronize()
+        bad = torch.isnan(y)
+        assert bad[rows // 2].all() and int(bad.sum()) == 70
+        op.close()
+
+
+@pytest.mark.parametrize("rows", [4, 300])
+def test_no_rows_and_a_graph(rows):
+    import torch
+    rng = np.random.default_rng(3)
+    w = rng.standard_normal((130, 512)).astype(np.float32)
+    op = binding.Linear8(binding.make_linear8_config(512, 130, True), w)
+    _, _, x8, sx = _rows8(torch, rng.standard_normal((rows, 512)))
+    y = torch.empty(rows, 130, dtype=torch.bfloat16, device="cuda:0")
+    op.run_device(x8[:0], sx[:0], y[:0])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=op.stream):
+        op.run_device(x8, sx, y)
+    for k in range(3):
+        _, _, a, b = _rows8(torch, rng.standard_normal((rows, 512)))
+        x8.view(torch.uint8).copy_(a.view(torch.uint8))
+        sx.view(torch.uint8).copy_(b.view(torch.uint8))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(op.stream):
+            g.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        op.run_device(x8, sx, y)
+        torch.cuda.synchronize()
+        assert torch.equal(got, y), k
+    op.close()
