@@ -33,7 +33,7 @@ struct Layout {
 Layout layout_of(const tts_linear8_config& c)
 {
     Layout l;
-    l.tiles = (c.out_dim + 15) / 16;
+    l.tiles = channel_tiles(c.out_dim);
     l.blocks = width8(c.in_dim) / E8_BLOCK;
     l.words = scale_columns(c.in_dim) / 4;
     Carver a;
@@ -103,6 +103,7 @@ extern "C" int tts_linear8_create(const tts_linear8_config* cfg, const float* w,
     OnDevice on(device);
     HIP_TRY(on.err);
     HIP_TRY(hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, device));
+    HIP_TRY(allow_linear8());
     // the arena's contents, as one host copy
     std::unique_ptr<uint8_t[]> host(new (std::nothrow) uint8_t[lay.total]());
     tts_linear8* p = new (std::nothrow) tts_linear8();
@@ -114,6 +115,7 @@ extern "C" int tts_linear8_create(const tts_linear8_config* cfg, const float* w,
     memset(host.get() + lay.sw, 127, (size_t)lay.tiles * lay.words * 64);
     for (int n = 0; n < N; ++n) {
         const float* row = w + (size_t)n * K;
+        const int t = channel_tile(n), r = channel_row(n);
         for (int b = 0; b < lay.blocks; ++b) {
             const int k0 = b * E8_BLOCK, kn = K - k0 < E8_BLOCK ? K - k0 : E8_BLOCK;
             float m = 0;
@@ -122,13 +124,13 @@ extern "C" int tts_linear8_create(const tts_linear8_config* cfg, const float* w,
                 if (a > m && a <= 3.402823466e38f) m = a;
             }
             const int byte = scale_byte(m);
-            host[lay.sw + (((size_t)(n / 16) * lay.words + b / 4) * 16 + n % 16) * 4 + b % 4] = (uint8_t)byte;
+            host[lay.sw + (((size_t)t * lay.words + b / 4) * 16 + r) * 4 + b % 4] = (uint8_t)byte;
             const uint32_t bits = (uint32_t)(254 - byte) << 23;
             float by;
             memcpy(&by, &bits, 4);
-            uint8_t* tile = host.get() + lay.w + ((size_t)(n / 16) * lay.blocks + b) * 2048;
+            uint8_t* tile = host.get() + lay.w + ((size_t)t * lay.blocks + b) * 2048;
             for (int k = 0; k < kn; ++k) {
-                const int half = k / 64, lane = (k % 64) / 16 * 16 + n % 16;
+                const int half = k / 64, lane = (k % 64) / 16 * 16 + r;
                 tile[half * 1024 + lane * 16 + k % 16] = host_f2e4m3(row[k0 + k] * by);
             }
         }

@@ -33,6 +33,7 @@ hipError_t launch_norm(const NormArgs& a, bool, bool, int, hipStream_t)
     devices_seen = current;
     return call("launch");
 }
+hipError_t allow_linear8() { return call("allow"); }
 hipError_t launch_linear8(const Linear8Args& a, bool, int, hipStream_t)
 {
     ++launches;
