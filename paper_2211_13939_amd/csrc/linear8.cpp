@@ -27,19 +27,19 @@ int check(const tts_linear8_config* c)
 }
 
 struct Layout {
-    int tiles, blocks, words;
+    int units, blocks, words;
     size_t w, sw, bias, total;
 };
 Layout layout_of(const tts_linear8_config& c)
 {
     Layout l;
-    l.tiles = channel_tiles(c.out_dim);
+    l.units = channel_units(c.out_dim);
     l.blocks = width8(c.in_dim) / E8_BLOCK;
     l.words = scale_columns(c.in_dim) / 4;
     Carver a;
-    l.w = a.take((size_t)l.tiles * l.blocks * 2048);
-    l.sw = a.take((size_t)l.tiles * l.words * 64);
-    l.bias = a.take((size_t)l.tiles * 64);
+    l.w = a.take((size_t)l.units * l.blocks * 4096);
+    l.sw = a.take((size_t)l.units * l.words * 128);
+    l.bias = a.take((size_t)l.units * 128);
     l.total = a.off;
     return l;
 }
@@ -112,10 +112,10 @@ extern "C" int tts_linear8_create(const tts_linear8_config* cfg, const float* w,
         return fail(TTS_E_INVAL, "out of host memory");
     }
     const int K = cfg->in_dim, N = cfg->out_dim;
-    memset(host.get() + lay.sw, 127, (size_t)lay.tiles * lay.words * 64);
+    memset(host.get() + lay.sw, 127, (size_t)lay.units * lay.words * 128);
     for (int n = 0; n < N; ++n) {
         const float* row = w + (size_t)n * K;
-        const int t = channel_tile(n), r = channel_row(n);
+        const int u = channel_unit(n), r = channel_row(n);
         for (int b = 0; b < lay.blocks; ++b) {
             const int k0 = b * E8_BLOCK, kn = K - k0 < E8_BLOCK ? K - k0 : E8_BLOCK;
             float m = 0;
@@ -124,15 +124,12 @@ extern "C" int tts_linear8_create(const tts_linear8_config* cfg, const float* w,
                 if (a > m && a <= 3.402823466e38f) m = a;
             }
             const int byte = scale_byte(m);
-            host[lay.sw + (((size_t)t * lay.words + b / 4) * 16 + r) * 4 + b % 4] = (uint8_t)byte;
+            host[lay.sw + (((size_t)u * lay.words + b / 4) * 32 + r) * 4 + b % 4] = (uint8_t)byte;
             const uint32_t bits = (uint32_t)(254 - byte) << 23;
             float by;
             memcpy(&by, &bits, 4);
-            uint8_t* tile = host.get() + lay.w + ((size_t)t * lay.blocks + b) * 2048;
-            for (int k = 0; k < kn; ++k) {
-                const int half = k / 64, lane = (k % 64) / 16 * 16 + r;
-                tile[half * 1024 + lane * 16 + k % 16] = host_f2e4m3(row[k0 + k] * by);
-            }
+            uint8_t* unit = host.get() + lay.w + ((size_t)u * lay.blocks + b) * 4096;
+            for (int k = 0; k < kn; ++k) unit[(k / 64 * 2 + k / 16 % 2) * 1024 + (k / 32 % 2 * 32 + r) * 16 + k % 16] = host_f2e4m3(row[k0 + k] * by);
         }
         if (bias) memcpy(host.get() + lay.bias + (size_t)n * 4, bias + n, 4);
     }

@@ -1,10 +1,9 @@
 // The product of 8-bit rows with 8-bit weights, a power of two for each 128 columns of either: y = x w^T + bias.
 //
-// A matrix instruction of 16 x 16 results takes 128 columns, a block, and both blocks' scales, so that a block costs no work beside it.
-// Channels are the instruction's rows and rows of x its columns: a lane ends with four neighbouring channels of one row.  Row 4 g + j of the t-th of
-// four tiles is channel 16 g + 4 t + j of their 64, so that with all four a lane has 16 neighbouring channels and a row's 64 are stored
-// together.  An operand is 32 bytes a lane: of row l % 16 the 16 bytes from column 16 * (l / 16) of either half of the block; both operands share
-// this map, so the order in which the instruction walks the columns does not matter.
+// A matrix instruction takes whole blocks of columns or half ones, and both operands' scales, so that a block costs no work beside it.  Channels are
+// the instruction's rows and rows of x its columns: a lane ends with neighbouring channels of one row.  Weights lie in units of 32
+// channels and 64 columns, as the 32 x 32 instruction takes them: 32 bytes a lane, of row l % 32 the columns from 32 * (l / 32) on.  Row 8 a + 4 h + j of
+// the t-th of two units is channel 32 h + 16 t + 4 a + j of the 64: a lane of that instruction has 16 neighbouring channels of a unit.
 #include "operator_kernels.h"
 #include "mfma.h"
 
@@ -25,10 +24,12 @@ template <bool EXACT> struct Operand;
 template <> struct Operand<false> {
     Frag8 f;
     int scale;
+    Operand() = default;
     __device__ __forceinline__ Operand(const Frag8& v, uint32_t byte) : f(v), scale((int)byte) {}
 };
 template <> struct Operand<true> {
     bf16x8 part[4];
+    Operand() = default;
     __device__ __forceinline__ Operand(const Frag8& v, uint32_t byte)
     {
         const float by = __uint_as_float(byte << 23);
@@ -46,9 +47,15 @@ template <> struct Operand<true> {
         }
     }
 };
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+// 16 x 16 results of 128 columns, or 32 x 32 of 64
 __device__ __forceinline__ floatx4 product(const Operand<false>& a, const Operand<false>& b, floatx4 acc)
 {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(a.f), operand(b.f), acc, 0, 0, 0, a.scale, 0, b.scale);
+}
+__device__ __forceinline__ floatx16 product(const Operand<false>& a, const Operand<false>& b, floatx16 acc)
+{
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(a.f), operand(b.f), acc, 0, 0, 0, a.scale, 0, b.scale);
 }
 __device__ __forceinline__ floatx4 product(const Operand<true>& a, const Operand<true>& b, floatx4 acc)
 {
@@ -56,9 +63,15 @@ __device__ __forceinline__ floatx4 product(const Operand<true>& a, const Operand
     for (int q = 0; q < 4; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.part[q], b.part[q], acc, 0, 0, 0);
     return acc;
 }
+__device__ __forceinline__ floatx16 product(const Operand<true>& a, const Operand<true>& b, floatx16 acc)
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.part[q], b.part[q], acc, 0, 0, 0);
+    return acc;
+}
 // In front of the first other use of accumulators.  The compiler has placed reads of the scaled instructions' results too few cycles behind
 // them where a branch lay between (garbage, seen on a loop that copied its accumulator); 32 cycles are what the longest takes.
-template <int N> __device__ __forceinline__ void settle(floatx4 (&acc)[N])
+template <typename V, int N> __device__ __forceinline__ void settle(V (&acc)[N])
 {
     asm volatile("s_nop 15\n\ts_nop 15" : "+v"(acc[0]));
 #pragma unroll
@@ -82,54 +95,44 @@ template <typename YT> __device__ __forceinline__ void store_four(const Linear8A
     }
 }
 
-// Few rows: the weights are what there is to read.  A workgroup forms 16 channels of up to 16 * MT rows; its waves take blocks in turn, straight from
-// memory into registers, and add their sums up through LDS in their order.
+// Up to 16 rows: the weights are what there is to read.  A workgroup forms 16 channels; its waves take blocks in turn, straight from memory into
+// registers, and add their sums up through LDS in their order.
 constexpr int FEW_WAVES = 8;
-template <typename YT, int MT> __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear8_few(Linear8Args p)
+template <typename YT> __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear8_few(Linear8Args p)
 {
     constexpr bool EXACT = sizeof(YT) == 4;
-    __shared__ floatx4 red[FEW_WAVES][MT][64];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
-    const int tiles = channel_tiles(p.out_dim), tile = blockIdx.x % tiles, row0 = blockIdx.x / tiles * 16 * MT;
-    const int width = p.blocks * E8_BLOCK, words = (p.blocks + 3) / 4;
-    const uint4* w = p.w + (size_t)tile * p.blocks * 128 + lane;
-    const uint32_t* sw = p.sw + (size_t)tile * words * 16 + (lane & 15);
-    const uint8_t* x[MT];
-    const uint8_t* sx[MT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const size_t row = min(row0 + 16 * m + (lane & 15), p.rows - 1);
-        x[m] = p.x8 + row * width + 16 * (lane >> 4);
-        sx[m] = p.sx + row * words * 4;
-    }
-    floatx4 acc[MT] = {};
-#pragma unroll 2
+    __shared__ floatx4 red[FEW_WAVES][64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, g = lane >> 4;
+    const int half = blockIdx.x, row = lane & 15, words = (p.blocks + 3) / 4;
+    // the 16 x 16 instruction's operand, 32 columns from 32 g on, from two units of columns
+    const uint4* w = p.w + ((size_t)(half >> 1) * p.blocks * 2 + (g >> 1)) * 128 + 32 * (g & 1) + 16 * (half & 1) + row;
+    const uint32_t* sw = p.sw + (size_t)(half >> 1) * words * 32 + 16 * (half & 1) + row;
+    const uint8_t* x = p.x8 + (size_t)min(row, p.rows - 1) * p.blocks * E8_BLOCK + 32 * g;
+    const uint8_t* sx = p.sx + (size_t)min(row, p.rows - 1) * words * 4;
+    floatx4 acc[1] = {};
     for (int b = wave; b < p.blocks; b += FEW_WAVES) {
-        const Frag8 wf = {w[(size_t)b * 128], w[(size_t)b * 128 + 64]};
-        const uint32_t ws = sw[b / 4 * 16] >> (8 * (b & 3)) & 255;
-        const Operand<EXACT> a(wf, ws);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const uint8_t* at = x[m] + (size_t)b * E8_BLOCK;
-            const Frag8 xf = {*reinterpret_cast<const uint4*>(at), *reinterpret_cast<const uint4*>(at + 64)};
-            acc[m] = product(a, Operand<EXACT>(xf, sx[m][b]), acc[m]);
-        }
+        const Frag8 wf = {w[(size_t)b * 256], w[(size_t)b * 256 + 64]};
+        const uint8_t* at = x + (size_t)b * E8_BLOCK;
+        const Frag8 xf = {*reinterpret_cast<const uint4*>(at), *reinterpret_cast<const uint4*>(at + 16)};
+        acc[0] = product(Operand<EXACT>(wf, sw[b / 4 * 32] >> (8 * (b & 3)) & 255), Operand<EXACT>(xf, sx[b]), acc[0]);
     }
     settle(acc);
-#pragma unroll
-    for (int m = 0; m < MT; ++m) red[wave][m][lane] = acc[m];
+    red[wave][lane] = acc[0];
     __syncthreads();
-    if (wave < MT) {
-        const int n0 = tile / 4 * 64 + 16 * (lane >> 4) + 4 * (tile & 3);
+    if (wave == 0) {
+        const int n0 = half / 4 * 64 + 32 * (g & 1) + 16 * (half >> 1 & 1) + 4 * (2 * (half & 1) + (g >> 1));
         floatx4 y = *reinterpret_cast<const floatx4*>(p.bias + n0);
 #pragma unroll
-        for (int i = 0; i < FEW_WAVES; ++i) y += red[i][wave][lane];
-        store_four<YT>(p, row0 + 16 * wave + (lane & 15), n0, y);
+        for (int i = 0; i < FEW_WAVES; ++i) y += red[i][lane];
+        store_four<YT>(p, row, n0, y);
     }
 }
 
-// Many rows: tiles of 16 * TN * WN channels and 16 * TM * WM rows, a block of columns of both in LDS while the next one is on its way there
-// (16 bytes a lane straight from memory, in operand order: the loads place them, no exchange and no conflict is left).
+// Many rows: tiles of 32 * TN * WN channels and 32 * TM * WM rows, in steps of 64 * SUB columns.  A step of both operands lies in LDS while the next
+// STEPS - 1 are on their way there, 16 bytes a lane straight from memory; one barrier a step.  Weights lie in operand order.  Of x four
+// lanes bring the 64 bytes of a row (lanes of rows apart, as the operand has them, take a cycle of the load path each: 256 x 256 tiles of
+// 16384 x 4096 x 4096 in 277 us), each the quarter that its place is for: rows' quarters change places every four rows, so that the
+// operand's reads of 16 bytes find all banks.
 //
 // These loads are written out: of the builtin the compiler does not know which of two buffers it fills, and waits for it in front of every read of the
 // other.  They have no registers to come back to; what they bring is there behind arrived().  (m0 has no other user in these kernels.)
@@ -139,192 +142,350 @@ template <int BYTES> __device__ __forceinline__ void to_lds(const uint8_t* base,
     if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
     else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
 }
-// What all waves brought is in LDS, and all have read what they needed.
-__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All but the last N loads of every wave are there, and all waves have read what they needed.
+template <int N> __device__ __forceinline__ void arrived()
+{
+    static_assert(N < 64, "the counter has six bits");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
 
-// The scale's byte J of a word
-template <int J> __device__ __forceinline__ floatx4 product_of(const Frag8& a, uint32_t sa, const Frag8& b, uint32_t sb, floatx4 acc)
+// 16 neighbouring channels of a row
+struct __attribute__((packed, aligned(2))) Eight16 { uint32_t w[4]; };
+template <typename YT> __device__ __forceinline__ void store_sixteen(const Linear8Args& p, int row, int n0, const floatx16& v)
 {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(a), operand(b), acc, 0, 0, J, (int)sa, J, (int)sb);
+    if (row >= p.rows || n0 >= p.out_dim) return;
+    YT* y = static_cast<YT*>(p.y) + row * p.y_stride + n0;
+    if (n0 + 16 <= p.out_dim) {
+        if constexpr (sizeof(YT) == 2) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 8)
+                *reinterpret_cast<Eight16*>(y + i) = Eight16{{pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]), pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7])}};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<Four32*>(y + i) = Four32{{v[i], v[i + 1], v[i + 2], v[i + 3]}};
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 15; ++i)
+            if (n0 + i < p.out_dim) y[i] = from_float<YT>(v[i]);
+    }
 }
 
-template <typename YT, int TN, int TM, int WN, int WM> struct Many {
+template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS> struct Many {
     static constexpr bool EXACT = sizeof(YT) == 4;
-    static constexpr int WAVES = WN * WM, NT = TN * WN, MT = TM * WM;            // tiles of a workgroup
-    static constexpr int STAGE = (NT + MT) * 2048, SCALES = (NT + MT) * 64, LDS = 2 * STAGE + 2 * SCALES;
-    static_assert(NT * 2 % WAVES == 0 && MT * 2 % WAVES == 0 && (NT + MT) == 4 * WAVES && NT % 4 == 0, "shares of the waves");
+    static constexpr int WAVES = WN * WM, NT = TN * WN, MT = TM * WM;            // units of a workgroup
+    static constexpr int PART = (NT + MT) * 2048, STEP = SUB * PART, SCALES = (NT + MT) * 128, LDS = STEPS * STEP + 2 * SCALES;
+    static constexpr int W_LOADS = SUB * NT * 2 / WAVES, X_LOADS = SUB * MT * 2 / WAVES, LOADS = W_LOADS + X_LOADS;      // of a wave a step
+    static constexpr int S_LOADS = ((NT + MT) / 2 + WAVES - 1) / WAVES;                      // ... every four blocks
+    static_assert(W_LOADS * WAVES == SUB * NT * 2 && X_LOADS * WAVES == SUB * MT * 2 && SUB <= 2 && NT % 2 == 0 && MT % 2 == 0, "shares of the waves");
     const Linear8Args& p;
-    uint8_t* lds;
-    int wave, lane, wn, wm, tile0, row0;
-    const uint8_t *w_at[NT * 2 / WAVES], *x_at;          // this wave's share of a stage
-    uint32_t x_off[MT * 2 / WAVES];
-    const uint8_t* s_base;                               // of the scales that it brings
-    uint32_t s_off, s_step, lds_at;
-    floatx4 acc[TN * TM] = {};
+    int wave, lane, wn, wm, unit0, row0;
+    uint32_t lds_at;
+    const uint8_t *w_at[W_LOADS], *x_at, *s_base[S_LOADS];      // this wave's share of a step, and of the scales
+    uint32_t x_off[X_LOADS], s_off[S_LOADS], s_step[S_LOADS];
+    const uint8_t* lds;
+    floatx16 acc[TN * TM] = {};
 
-    __device__ __forceinline__ Many(const Linear8Args& a, uint8_t* l, int n_tile, int m_tile) : p(a), lds(l)
+    __device__ __forceinline__ Many(const Linear8Args& a, const uint8_t* l, int n_tile, int m_tile) : p(a), lds(l)
     {
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         lane = threadIdx.x & 63;
         wn = wave % WN;
         wm = wave / WN;
-        tile0 = n_tile * NT;
-        row0 = m_tile * MT * 16;
-        const int tiles = channel_tiles(p.out_dim), words = (p.blocks + 3) / 4;
+        unit0 = n_tile * NT;
+        row0 = m_tile * MT * 32;
+        const int units = channel_units(p.out_dim), words = (p.blocks + 3) / 4;
         const uint32_t width = p.blocks * E8_BLOCK;
         const uint8_t* w = reinterpret_cast<const uint8_t*>(p.w);
 #pragma unroll
-        for (int i = 0; i < NT * 2 / WAVES; ++i) {
-            const int c = wave + i * WAVES;
-            w_at[i] = w + ((size_t)min(tile0 + c / 2, tiles - 1) * p.blocks * 128 + (c & 1) * 64) * 16;
+        for (int i = 0; i < W_LOADS; ++i) {
+            const int c = wave + i * WAVES, sub = c / (2 * NT), u = c % (2 * NT) / 2;
+            w_at[i] = w + ((size_t)min(unit0 + u, units - 1) * p.blocks * 4 + 2 * sub + (c & 1)) * 1024;
         }
         x_at = p.x8 + (size_t)row0 * width;
 #pragma unroll
-        for (int i = 0; i < MT * 2 / WAVES; ++i) {
-            const int c = wave + i * WAVES;
-            x_off[i] = (uint32_t)min(c / 2 * 16 + (lane & 15), p.rows - 1 - row0) * width + (c & 1) * 64 + 16 * (lane >> 4);
+        for (int i = 0; i < X_LOADS; ++i) {
+            const int c = wave + i * WAVES, sub = c / (2 * MT), r = c % (2 * MT) * 16;
+            x_off[i] = (uint32_t)min(r + (lane >> 2), p.rows - 1 - row0) * width + 64 * sub + 16 * ((lane ^ (lane >> 4)) & 3);
         }
-        // a wave brings the scales of four tiles
-        if (4 * wave < NT) {
-            s_base = reinterpret_cast<const uint8_t*>(p.sw + (size_t)min(tile0 + 4 * wave, tiles - 4) * words * 16);
-            s_off = (uint32_t)((lane >> 4) * words * 16 + (lane & 15)) * 4;
-            s_step = 64;
-        } else {
-            s_base = p.sx + (size_t)row0 * words * 4;
-            s_off = (uint32_t)min((4 * wave - NT) * 16 + lane, p.rows - 1 - row0) * words * 4;
-            s_step = 4;
+        // a load brings the scales of two units
+#pragma unroll
+        for (int i = 0; i < S_LOADS; ++i) {
+            const int c = 2 * (wave + i * WAVES);
+            if (c < NT) {
+                s_base[i] = reinterpret_cast<const uint8_t*>(p.sw + (size_t)min(unit0 + c, units - 2) * words * 32);
+                s_off[i] = (uint32_t)((lane >> 5) * words * 32 + (lane & 31)) * 4;
+                s_step[i] = 128;
+            } else {
+                s_base[i] = p.sx + (size_t)row0 * words * 4;
+                s_off[i] = (uint32_t)min((c - NT) * 32 + lane, p.rows - 1 - row0) * words * 4;
+                s_step[i] = 4;
+            }
         }
         lds_at = lds_address(lds);
     }
-    __device__ __forceinline__ void bring(int b, int buf) const
+    __device__ __forceinline__ void bring(int step, int slot) const
     {
-        const uint32_t to = lds_at + buf * STAGE + wave * 1024;
+        const uint32_t to = lds_at + slot * STEP;
 #pragma unroll
-        for (int i = 0; i < NT * 2 / WAVES; ++i) to_lds<16>(w_at[i] + (size_t)b * 2048, lane * 16, to + i * WAVES * 1024);
+        for (int i = 0; i < W_LOADS; ++i) {
+            const int c = wave + i * WAVES;
+            to_lds<16>(w_at[i] + (size_t)step * (2048 * SUB), lane * 16, to + c / (2 * NT) * PART + c % (2 * NT) * 1024);
+        }
 #pragma unroll
-        for (int i = 0; i < MT * 2 / WAVES; ++i) to_lds<16>(x_at + (size_t)b * E8_BLOCK, x_off[i], to + NT * 2048 + i * WAVES * 1024);
-    }
-    __device__ __forceinline__ void bring_scales(int word, int buf) const { to_lds<4>(s_base + (size_t)word * s_step, s_off, lds_at + 2 * STAGE + buf * SCALES + wave * 256); }
-    __device__ __forceinline__ Frag8 frag(int buf, int tile) const
-    {
-        const uint4* at = reinterpret_cast<const uint4*>(lds + buf * STAGE + tile * 2048) + lane;
-        return Frag8{at[0], at[64]};
-    }
-    template <int J> __device__ __forceinline__ void block(const uint32_t (&sw)[TN], const uint32_t (&sx)[TM])
-    {
-        constexpr int buf = J & 1;
-        if constexpr (EXACT) {
-            bf16x8 x[TM][4];
-#pragma unroll
-            for (int m = 0; m < TM; ++m) {
-                const Operand<true> o(frag(buf, NT + wm * TM + m), sx[m] >> (8 * J) & 255);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) x[m][q] = o.part[q];
-            }
-#pragma unroll
-            for (int n = 0; n < TN; ++n) {
-                const Operand<true> o(frag(buf, wn * TN + n), sw[n] >> (8 * J) & 255);
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int m = 0; m < TM; ++m) acc[n * TM + m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(o.part[q], x[m][q], acc[n * TM + m], 0, 0, 0);
-            }
-        } else {
-            Frag8 x[TM];
-#pragma unroll
-            for (int m = 0; m < TM; ++m) x[m] = frag(buf, NT + wm * TM + m);
-#pragma unroll
-            for (int n = 0; n < TN; ++n) {
-                const Frag8 w = frag(buf, wn * TN + n);
-#pragma unroll
-                for (int m = 0; m < TM; ++m) acc[n * TM + m] = product_of<J>(w, sw[n], x[m], sx[m], acc[n * TM + m]);
-            }
+        for (int i = 0; i < X_LOADS; ++i) {
+            const int c = wave + i * WAVES;
+            to_lds<16>(x_at + (size_t)step * (64 * SUB), x_off[i], to + c / (2 * MT) * PART + NT * 2048 + c % (2 * MT) * 1024);
         }
     }
-    // block 4 * word + J of the columns; false: it was the last
-    template <int J> __device__ __forceinline__ bool turn(int word, const uint32_t (&sw)[TN], const uint32_t (&sx)[TM])
+    __device__ __forceinline__ void bring_scales(int word) const
     {
-        const int b = 4 * word + J;
-        if (b + 1 < p.blocks) bring(b + 1, (J + 1) & 1);
-        block<J>(sw, sx);
-        arrived();
-        return b + 1 < p.blocks;
+#pragma unroll
+        for (int i = 0; i < S_LOADS; ++i)
+            if (2 * (wave + i * WAVES) < NT + MT) to_lds<4>(s_base[i] + (size_t)word * s_step[i], s_off[i], lds_at + STEPS * STEP + (word & 1) * SCALES + (wave + i * WAVES) * 256);
+    }
+    __device__ __forceinline__ Frag8 w_frag(int part, int unit) const
+    {
+        const uint4* at = reinterpret_cast<const uint4*>(lds + part + unit * 2048) + lane;
+        return Frag8{at[0], at[64]};
+    }
+    __device__ __forceinline__ Frag8 x_frag(int part, int unit) const
+    {
+        const uint4* at = reinterpret_cast<const uint4*>(lds + part + (NT + unit) * 2048) + 4 * (lane & 31);
+        const int q = 2 * (lane >> 5) ^ (lane >> 2 & 3);
+        return Frag8{at[q], at[q ^ 1]};
+    }
+    __device__ __forceinline__ void multiply(int block, int part, const uint32_t (&sw)[TN], const uint32_t (&sx)[TM])
+    {
+        const int shift = 8 * (block & 3);               // a word holds the scales of four blocks
+        Operand<EXACT> x[TM];
+#pragma unroll
+        for (int m = 0; m < TM; ++m) x[m] = Operand<EXACT>(x_frag(part, wm * TM + m), sx[m] >> shift & 255);
+        Frag8 w = w_frag(part, wn * TN);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 + 2 * TM, 0);
+#pragma unroll
+        for (int n = 0; n < TN; ++n) {
+            Frag8 next;
+            if (n + 1 < TN) next = w_frag(part, wn * TN + n + 1);
+            const Operand<EXACT> a(w, sw[n] >> shift & 255);
+#pragma unroll
+            for (int m = 0; m < TM; ++m) acc[n * TM + m] = product(a, x[m], acc[n * TM + m]);
+            // a unit's products behind the next one's reads: left alone, the compiler puts each read in front of its use
+            if (n + 1 < TN) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, (EXACT ? 4 : 1) * TM, 0);
+            if (n + 1 < TN) w = next;
+        }
     }
     __device__ __forceinline__ void run()
     {
-        bring_scales(0, 0);
-        bring(0, 0);
-        arrived();
-        for (int word = 0;; ++word) {
-            if (4 * word + 4 < p.blocks) bring_scales(word + 1, (word + 1) & 1);
-            uint32_t sw[TN], sx[TM];
-            const uint32_t* s = reinterpret_cast<const uint32_t*>(lds + 2 * STAGE + (word & 1) * SCALES) + (lane & 15);
+        constexpr int PER_WORD = 8 / SUB;
+        const int steps = 2 / SUB * p.blocks;
+        bring_scales(0);
+        for (int i = 0; i < STEPS - 1 && i < steps; ++i) bring(i, i);
+        uint32_t sw[TN], sx[TM];
+        for (int step = 0, slot = 0, free = STEPS - 1; step < steps; ++step) {
+            // (the steps behind this one that are on their way: STEPS - 2 but at the end)
+            if (step + STEPS - 2 < steps) arrived<(STEPS - 2) * LOADS>();
+            else arrived<0>();
+            if (step % PER_WORD == 0) {
+                const uint32_t* s = reinterpret_cast<const uint32_t*>(lds + STEPS * STEP + (step / PER_WORD & 1) * SCALES) + (lane & 31);
 #pragma unroll
-            for (int n = 0; n < TN; ++n) sw[n] = s[(wn * TN + n) * 16];
+                for (int n = 0; n < TN; ++n) sw[n] = s[(wn * TN + n) * 32];
 #pragma unroll
-            for (int m = 0; m < TM; ++m) sx[m] = s[(NT + wm * TM + m) * 16];
-            if (!turn<0>(word, sw, sx) || !turn<1>(word, sw, sx) || !turn<2>(word, sw, sx) || !turn<3>(word, sw, sx)) break;
+                for (int m = 0; m < TM; ++m) sx[m] = s[(NT + wm * TM + m) * 32];
+                if (step + PER_WORD < steps) bring_scales(step / PER_WORD + 1);
+            }
+            if (step + STEPS - 1 < steps) bring(step + STEPS - 1, free);
+#pragma unroll
+            for (int sub = 0; sub < SUB; ++sub) multiply(SUB == 2 ? step : step >> 1, slot * STEP + sub * PART, sw, sx);
+            free = slot;                                  // (the slot that the step before this one was in)
+            slot = slot + 1 == STEPS ? 0 : slot + 1;
         }
         settle(acc);
 #pragma unroll
         for (int n = 0; n < TN; ++n) {
-            const int t = tile0 + wn * TN + n, n0 = t / 4 * 64 + 16 * (lane >> 4) + 4 * (t & 3);
-            const floatx4 bias = n0 < p.out_dim ? *reinterpret_cast<const floatx4*>(p.bias + n0) : floatx4{0.f, 0.f, 0.f, 0.f};
+            const int u = unit0 + wn * TN + n, n0 = u / 2 * 64 + 32 * (lane >> 5) + 16 * (u & 1);
+            floatx16 bias = {};
+            if (n0 < p.out_dim) bias = *reinterpret_cast<const floatx16*>(p.bias + n0);
 #pragma unroll
-            for (int m = 0; m < TM; ++m) store_four<YT>(p, row0 + (wm * TM + m) * 16 + (lane & 15), n0, acc[n * TM + m] + bias);
+            for (int m = 0; m < TM; ++m) store_sixteen<YT>(p, row0 + (wm * TM + m) * 32 + (lane & 31), n0, acc[n * TM + m] + bias);
         }
     }
 };
 
-template <typename YT, int TN, int TM, int WN, int WM> __global__ __launch_bounds__(64 * WN * WM, WN * WM / 4) void k_linear8_many(Linear8Args p, int n_tiles, int m_tiles)
+template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS>
+__global__ __launch_bounds__(64 * WN * WM, WN * WM / 4) void k_linear8_many(Linear8Args p, int n_tiles, int m_tiles)
 {
     extern __shared__ __align__(16) uint8_t lds[];
     // Workgroups are dealt to the eight XCDs in turn; an XCD takes a run of tiles, 4 rows of tiles high, so that its L2 holds what they share.
     const int total = n_tiles * m_tiles, per = (total + 7) / 8;
     const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if (id >= total || (int)(blockIdx.x >> 3) >= per) return;
+    if (id >= total) return;
     const int band = id / (4 * n_tiles), in_band = id - band * 4 * n_tiles, high = min(4, m_tiles - 4 * band);
-    Many<YT, TN, TM, WN, WM> many(p, lds, in_band / high, 4 * band + in_band % high);
+    Many<YT, TN, TM, WN, WM, SUB, STEPS> many(p, lds, in_band / high, 4 * band + in_band % high);
     many.run();
 }
 
-template <typename YT, int TN, int TM, int WN, int WM> hipError_t allow()
+// In between: 32 channels and 32 * TM rows a workgroup, whose waves take steps of 64 columns in turn, each through a ring in LDS of its own (no
+// barrier until their sums meet).  A wave's i-th step has its scales in word i.
+constexpr int SPLIT_WAVES = 8;
+template <typename YT, int TM, int RING> struct Split {
+    static constexpr bool EXACT = sizeof(YT) == 4;
+    static constexpr int SLOT = (1 + TM) * 2048 + 256 * ((TM + 2) / 2), LOADS = 2 + 2 * TM + (TM + 2) / 2, LDS = SPLIT_WAVES * RING * SLOT;
+    static_assert(LDS >= SPLIT_WAVES * TM * 4096 && LDS <= 160 * 1024, "the sums meet in the rings");
+};
+// All but the last N loads of this wave are there.
+template <int N> __device__ __forceinline__ void brought()
 {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(k_linear8_many<YT, TN, TM, WN, WM>), hipFuncAttributeMaxDynamicSharedMemorySize, Many<YT, TN, TM, WN, WM>::LDS);
+    static_assert(N < 64, "the counter has six bits");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-template <typename YT, int TN, int TM, int WN, int WM> hipError_t go_many(const Linear8Args& a, hipStream_t s)
+__device__ __forceinline__ void lane_to_lds(const void* from, uint32_t to)
 {
-    using M = Many<YT, TN, TM, WN, WM>;
-    const int n_tiles = (channel_tiles(a.out_dim) + M::NT - 1) / M::NT, m_tiles = (a.rows + M::MT * 16 - 1) / (M::MT * 16);
-    hipLaunchKernelGGL((k_linear8_many<YT, TN, TM, WN, WM>), dim3((n_tiles * m_tiles + 7) / 8 * 8), dim3(64 * WN * WM), M::LDS, s, a, n_tiles, m_tiles);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
+}
+template <typename YT, int TM, int RING> __global__ __launch_bounds__(SPLIT_WAVES * 64, 2) void k_linear8_split(Linear8Args p)
+{
+    using S = Split<YT, TM, RING>;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
+    const int units = channel_units(p.out_dim), unit = blockIdx.x % units, row0 = blockIdx.x / units * 32 * TM;
+    const int words = (p.blocks + 3) / 4, steps = 2 * p.blocks;
+    const uint32_t width = p.blocks * E8_BLOCK;
+    const uint8_t* w_at = reinterpret_cast<const uint8_t*>(p.w) + (size_t)unit * p.blocks * 4096;
+    const uint8_t* x_at = p.x8 + (size_t)row0 * width;
+    uint32_t x_off[2 * TM];
+#pragma unroll
+    for (int c = 0; c < 2 * TM; ++c) x_off[c] = (uint32_t)min(c * 16 + (lane >> 2), p.rows - 1 - row0) * width + 16 * ((lane ^ (lane >> 4)) & 3);
+    // the scales: 32 channels' and 32 * TM rows', 64 a load
+    const uint8_t* s_at[(TM + 2) / 2];
+    int s_step[(TM + 2) / 2];
+#pragma unroll
+    for (int i = 0; i < (TM + 2) / 2; ++i) {
+        const int r = i * 64 + lane - 32;
+        s_at[i] = r < 0 ? reinterpret_cast<const uint8_t*>(p.sw + (size_t)unit * words * 32 + lane) : p.sx + (size_t)min(row0 + r, p.rows - 1) * words * 4;
+        s_step[i] = r < 0 ? 128 : 4;
+    }
+    uint8_t* ring = lds + wave * RING * S::SLOT;
+    const uint32_t ring_at = lds_address(ring);
+    const int turns = steps > wave ? (steps - wave + SPLIT_WAVES - 1) / SPLIT_WAVES : 0;
+    auto bring = [&](int turn) {
+        const uint32_t to = ring_at + turn % RING * S::SLOT;
+        const size_t step = (size_t)turn * SPLIT_WAVES + wave;
+        to_lds<16>(w_at + step * 2048, lane * 16, to);
+        to_lds<16>(w_at + step * 2048 + 1024, lane * 16, to + 1024);
+#pragma unroll
+        for (int c = 0; c < 2 * TM; ++c) to_lds<16>(x_at + step * 64, x_off[c], to + 2048 + c * 1024);
+#pragma unroll
+        for (int i = 0; i < (TM + 2) / 2; ++i) lane_to_lds(s_at[i] + turn * s_step[i], to + (1 + TM) * 2048 + i * 256);
+    };
+    floatx16 acc[TM] = {};
+    for (int i = 0; i < RING && i < turns; ++i) bring(i);
+    for (int turn = 0; turn < turns; ++turn) {
+        if (turn + RING <= turns) brought<(RING - 1) * S::LOADS>();
+        else brought<0>();
+        const uint8_t* slot = ring + turn % RING * S::SLOT;
+        const uint4* w = reinterpret_cast<const uint4*>(slot) + lane;
+        const uint4* x = reinterpret_cast<const uint4*>(slot + 2048) + 4 * (lane & 31);
+        const uint32_t* s = reinterpret_cast<const uint32_t*>(slot + (1 + TM) * 2048) + (lane & 31);
+        const int q = 2 * (lane >> 5) ^ (lane >> 2 & 3), shift = 8 * (wave >> 1 & 3);
+        const Frag8 wf = {w[0], w[64]};
+        const uint32_t ws = s[0];
+        Frag8 xf[TM];
+        uint32_t xs[TM];
+#pragma unroll
+        for (int m = 0; m < TM; ++m) {
+            xf[m] = Frag8{x[128 * m + q], x[128 * m + (q ^ 1)]};
+            xs[m] = s[32 + 32 * m];
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the slot is free)
+        if (turn + RING < turns) bring(turn + RING);
+        const Operand<S::EXACT> a(wf, ws >> shift & 255);
+#pragma unroll
+        for (int m = 0; m < TM; ++m) acc[m] = product(a, Operand<S::EXACT>(xf[m], xs[m] >> shift & 255), acc[m]);
+    }
+    settle(acc);
+    __syncthreads();                                              // (the rings are read)
+    float* sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int m = 0; m < TM; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[((wave * TM + m) * 16 + i) * 64 + lane] = acc[m][i];
+    __syncthreads();
+    for (int job = wave; job < 4 * TM; job += SPLIT_WAVES) {
+        const int m = job >> 2, i0 = 4 * (job & 3);
+        const int n0 = unit / 2 * 64 + 32 * (lane >> 5) + 16 * (unit & 1) + i0;
+        floatx4 y = n0 < p.out_dim ? *reinterpret_cast<const floatx4*>(p.bias + n0) : floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < SPLIT_WAVES; ++w)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] += sums[((w * TM + m) * 16 + i0 + i) * 64 + lane];
+        store_four<YT>(p, row0 + 32 * m + (lane & 31), n0, y);
+    }
+}
+template <typename YT, int TM, int RING> hipError_t allow_split()
+{
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(k_linear8_split<YT, TM, RING>), hipFuncAttributeMaxDynamicSharedMemorySize, Split<YT, TM, RING>::LDS);
+}
+template <typename YT, int TM, int RING> hipError_t go_split(const Linear8Args& a, hipStream_t s)
+{
+    constexpr int LDS = Split<YT, TM, RING>::LDS;
+    hipLaunchKernelGGL((k_linear8_split<YT, TM, RING>), dim3(channel_units(a.out_dim) * ((a.rows + 32 * TM - 1) / (32 * TM))), dim3(SPLIT_WAVES * 64), LDS, s, a);
+    return hipGetLastError();
+}
+
+template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS> hipError_t allow()
+{
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(k_linear8_many<YT, TN, TM, WN, WM, SUB, STEPS>), hipFuncAttributeMaxDynamicSharedMemorySize, Many<YT, TN, TM, WN, WM, SUB, STEPS>::LDS);
+}
+template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS> hipError_t go_many(const Linear8Args& a, hipStream_t s)
+{
+    using M = Many<YT, TN, TM, WN, WM, SUB, STEPS>;
+    const int n_tiles = (channel_units(a.out_dim) + M::NT - 1) / M::NT, m_tiles = (a.rows + M::MT * 32 - 1) / (M::MT * 32);
+    hipLaunchKernelGGL((k_linear8_many<YT, TN, TM, WN, WM, SUB, STEPS>), dim3((n_tiles * m_tiles + 7) / 8 * 8), dim3(64 * WN * WM), M::LDS, s, a, n_tiles, m_tiles);
     return hipGetLastError();
 }
 
 template <typename YT> hipError_t go(const Linear8Args& a, int n_cu, hipStream_t s)
 {
-    const int tiles = channel_tiles(a.out_dim);
-    const dim3 block(FEW_WAVES * 64);
-    if (a.rows <= 16) hipLaunchKernelGGL((k_linear8_few<YT, 1>), dim3(tiles), block, 0, s, a);
-    else if (a.rows <= 32) hipLaunchKernelGGL((k_linear8_few<YT, 2>), dim3(tiles), block, 0, s, a);
-    else if (a.rows <= 64) hipLaunchKernelGGL((k_linear8_few<YT, 4>), dim3(tiles), block, 0, s, a);
-    else {
-        const long long large = (long long)((tiles + 15) / 16) * ((a.rows + 255) / 256);
-        return large >= n_cu ? go_many<YT, 8, 4, 2, 4>(a, s) : go_many<YT, 4, 4, 2, 2>(a, s);
+    const int units = channel_units(a.out_dim);
+    // A few rows: memory's rate is what counts (8192 x 8192 weights 11.6 us, 5.8 TB/s).  Up to 16 of them the plain loads of x still cost less than
+    // a ring, unless the weights are many (16 rows, k_linear8_few / k_linear8_split: 1024 x 1024 2.8 / 3.2 us, 4096 x 4096 5.7 / 5.2, 8192 x 8192 15.7 /
+    // 12.3; 8 rows of 4096 x 4096 4.5 / 5.0).
+    if (a.rows <= 8 || (a.rows <= 16 && units * a.blocks <= 2048)) {
+        hipLaunchKernelGGL((k_linear8_few<YT>), dim3(2 * units), dim3(FEW_WAVES * 64), 0, s, a);
+        return hipGetLastError();
     }
-    return hipGetLastError();
+    // Otherwise the largest tile that leaves two workgroups for every compute unit: a larger one asks for fewer bytes, a smaller one has its latencies
+    // spread over more.  us, two-byte results, 32 x 32 split / 64 x 64 / 64 channels x 128 rows / 128 x 128 / 256 x 128: 512 x 1024 x 1024 4.5 / 4.8 / 5.6 /
+    // 7.8 / 12.5; 1024 x 2048 x 2048 17.6 / 8.6 / 9.7 / 12.6 / 20.5; 4096 x 1024 x 1024 - / 11.6 / 9.5 / 10.1 / 14.1; 4096 x 2048 x 2048 - / 31.4 / 28.0 / 22.7 /
+    // 24.9; 16384 x 1024 x 1024 - / 34.9 / 30.1 / 28.6 / 26.3; 16384 x 4096 x 4096 - / 423 / 352 / 275 / 244.
+    auto tiles = [&](int n, int m) { return (long long)((units + n - 1) / n) * ((a.rows + 32 * m - 1) / (32 * m)); };
+    const int enough = 2 * n_cu;
+    if (tiles(1, 1) <= enough) return go_split<YT, 1, 2>(a, s);
+    if (tiles(8, 4) >= enough) return go_many<YT, 4, 2, 2, 2, 1, 3>(a, s);
+    if (tiles(4, 4) >= enough) return go_many<YT, 2, 2, 2, 2, 2, 2>(a, s);
+    if (tiles(2, 4) >= enough) return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
+    return go_many<YT, 1, 1, 2, 2, 2, 3>(a, s);
 }
 
 }  // namespace
 
 // (more than 64 KB of LDS a workgroup has to be allowed, on each device)
+template <typename YT> static hipError_t allow_all()
+{
+    hipError_t e = allow_split<YT, 1, 2>();
+    if (e == hipSuccess) e = allow<YT, 4, 2, 2, 2, 1, 3>();
+    if (e == hipSuccess) e = allow<YT, 2, 2, 2, 2, 2, 2>();
+    if (e == hipSuccess) e = allow<YT, 1, 2, 2, 2, 2, 2>();
+    if (e == hipSuccess) e = allow<YT, 1, 1, 2, 2, 2, 3>();
+    return e;
+}
 hipError_t allow_linear8()
 {
-    hipError_t e = allow<bf16_t, 8, 4, 2, 4>();
-    if (e == hipSuccess) e = allow<bf16_t, 4, 4, 2, 2>();
-    if (e == hipSuccess) e = allow<float, 8, 4, 2, 4>();
-    if (e == hipSuccess) e = allow<float, 4, 4, 2, 2>();
-    return e;
+    const hipError_t e = allow_all<bf16_t>();
+    return e == hipSuccess ? allow_all<float>() : e;
 }
 
 hipError_t launch_linear8(const Linear8Args& a, bool y_bf16, int n_cu, hipStream_t s)

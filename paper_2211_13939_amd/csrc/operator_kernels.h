@@ -21,15 +21,15 @@ struct NormArgs {
 };
 hipError_t launch_norm(const NormArgs& a, bool x_bf16, bool res_bf16, int n_cu, hipStream_t s);
 
-// Channels lie in fours of tiles: row 4 g + j of the t-th is channel 16 g + 4 t + j of the 64.
-constexpr int channel_tiles(int channels) { return (channels + 63) / 64 * 4; }
-constexpr int channel_tile(int n) { return n / 64 * 4 + n / 4 % 4; }
-constexpr int channel_row(int n) { return n / 16 % 4 * 4 + n % 4; }
+// Channels lie in pairs of units of 32: row 8 a + 4 h + j of the t-th is channel 32 h + 16 t + 4 a + j of the 64.
+constexpr int channel_units(int channels) { return (channels + 63) / 64 * 2; }
+constexpr int channel_unit(int n) { return n / 64 * 2 + n / 16 % 2; }
+constexpr int channel_row(int n) { return n / 4 % 4 * 8 + n / 32 % 2 * 4 + n % 4; }
 struct Linear8Args {
     const uint8_t *x8, *sx;              // [rows][width8], [rows][scale_columns]
-    const uint4* w;                      // [tiles of 16 channels][blocks][2 halves][64 lanes] 16 bytes: lane l holds row l % 16 of the tile, columns 64 * half + 16 * (l / 16) ..
-    const uint32_t* sw;                  // [tiles of 16 channels][words of scales][16 rows]
-    const float* bias;                   // [channels], zeros if there is none
+    const uint4* w;                      // [units][halves of blocks][2][64 lanes] 16 bytes: the c-th of lane l holds row l % 32 of the unit, columns 32 * (l / 32) + 16 * c ..
+    const uint32_t* sw;                  // [units][words of scales][32 rows]
+    const float* bias;                   // [32 * units], zeros where there is none
     void* y;
     long long y_stride;
     int rows, out_dim, blocks;           // blocks: of 128 columns

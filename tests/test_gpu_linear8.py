@@ -34,7 +34,8 @@ def _want(xb, xs, w, bias, bf16):
 
 
 @pytest.mark.parametrize("rows,k,n", [(1, 1, 1), (1, 1024, 512), (2, 127, 15), (15, 128, 16), (16, 129, 17), (17, 640, 250), (32, 1000, 64), (33, 2048, 48),
-                                      (64, 512, 1024), (65, 384, 130), (128, 256, 256), (129, 1024, 257), (200, 1500, 511), (256, 128, 512), (257, 300, 1000), (777, 1000, 1111)])
+                                      (64, 512, 1024), (65, 384, 130), (128, 256, 256), (129, 1024, 257), (200, 1500, 511), (256, 128, 512), (257, 300, 1000), (777, 1000, 1111),
+                                      (9, 4096, 4100), (1030, 260, 1030), (4090, 200, 1000), (8190, 130, 1000), (16390, 140, 1000), (16384, 256, 1024)])
 @pytest.mark.parametrize("bf16", [False, True])
 def test_product_against_64_bits(rows, k, n, bf16):
     import torch
@@ -69,7 +70,7 @@ def test_rows_do_not_depend_on_their_batch(bf16):
     xb, xs, x8, sx = _rows8(torch, rng.standard_normal((600, 700)))
     op = binding.Linear8(binding.make_linear8_config(700, 300, bf16), w, stream=torch.cuda.current_stream())
     want, tol = _want(xb, xs, w, None, bf16)
-    for rows in (1, 3, 16, 40, 64, 100, 256, 600):
+    for rows in (1, 3, 9, 16, 40, 64, 100, 256, 600):
         y = torch.empty(rows, 300, dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda:0")
         again = torch.empty_like(y)
         op.run_device(x8[:rows], sx[:rows], y)

@@ -172,8 +172,8 @@ def test_linear8_refuses(lib):
 
 @pytest.mark.parametrize("n,k", [(1, 1), (16, 128), (70, 300), (33, 1100)])
 def test_linear8_weights_are_rounded_and_laid_out(lib, n, k):
-    """The arena against the definition: [tiles of 16 channels][blocks][2 halves][64 lanes] 16 bytes, then scales [tiles][words][16 rows], then the bias; row
-    4 g + j of the t-th of four tiles is channel 16 g + 4 t + j of the 64."""
+    """The arena against the definition: [units of 32 channels][steps of 64 columns][2][64 lanes] 16 bytes, the c-th of lane l of row l % 32 from column
+    32 * (l / 32) + 16 * c on; then scales [units][words][32 rows], then the bias.  Row 8 a + 4 h + j of the t-th of two units is channel 32 h + 16 t + 4 a + j."""
     lib.fake_reset()
     rng = np.random.default_rng(n + k)
     w = (rng.standard_normal((n, k)) * 2.0 ** rng.integers(-30, 30, (n, 1))).astype(np.float32)
@@ -184,19 +184,19 @@ def test_linear8_weights_are_rounded_and_laid_out(lib, n, k):
     bias = rng.standard_normal(n).astype(np.float32)
     m = Made(lib, "linear8", binding.make_linear8_config(k, n), _floats(w), _floats(bias))
     want, want_s = ref.round8(w.astype(np.float64))
-    tiles, blocks, words = -(-n // 64) * 4, ref.blocks_of(k), want_s.shape[1] // 4
-    size = tiles * blocks * 2048
-    c = np.arange(tiles * 16)
-    row = (c // 64 * 4 + c // 4 % 4) * 16 + c // 16 % 4 * 4 + c % 4        # where channel c lies
-    got = m.arena[:size].reshape(tiles, blocks, 2, 4, 16, 16)     # tile, block, half, column group, row, byte
-    got = got.transpose(0, 4, 1, 2, 3, 5).reshape(tiles * 16, blocks * 128)[row]
+    units, blocks, words = -(-n // 64) * 2, ref.blocks_of(k), want_s.shape[1] // 4
+    size = units * blocks * 4096
+    c = np.arange(units * 32)
+    row = (c // 64 * 2 + c // 16 % 2) * 32 + c // 4 % 4 * 8 + c // 32 % 2 * 4 + c % 4        # where channel c lies
+    got = m.arena[:size].reshape(units, 2 * blocks, 2, 2, 32, 16)           # unit, step, c, l / 32, row, byte
+    got = got.transpose(0, 4, 1, 3, 2, 5).reshape(units * 32, blocks * 128)[row]
     np.testing.assert_array_equal(got[:n], want)
     assert (got[n:] == 0).all()
     at = -(-size // 256) * 256
-    s = m.arena[at: at + tiles * words * 64].reshape(tiles, words, 16, 4).transpose(0, 2, 1, 3).reshape(tiles * 16, words * 4)[row]
+    s = m.arena[at: at + units * words * 128].reshape(units, words, 32, 4).transpose(0, 2, 1, 3).reshape(units * 32, words * 4)[row]
     np.testing.assert_array_equal(s[:n], want_s)
     assert (s[n:] == 127).all()
-    at += -(-tiles * words * 64 // 256) * 256
+    at += -(-units * words * 128 // 256) * 256
     np.testing.assert_array_equal(m.arena[at: at + 4 * n].view(np.float32), bias)
     m.close()
 
