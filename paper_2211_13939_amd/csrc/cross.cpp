@@ -24,11 +24,23 @@ int check(const tts_cross_config* c)
     return TTS_OK;
 }
 
+struct Layout { size_t parts, zeros, total; };
+Layout layout_of()
+{
+    Layout l;
+    Carver a;
+    l.parts = a.take(cross_parts_bytes());
+    l.zeros = a.take(256);
+    l.total = a.off;
+    return l;
+}
+
 }  // namespace
 
 struct tts_cross {
     tts_cross_config cfg;
     float* parts = nullptr;              // device
+    const void* zeros = nullptr;
     hipStream_t stream = nullptr;
     int device = 0, n_cu = 0;
 };
@@ -36,7 +48,7 @@ struct tts_cross {
 extern "C" size_t tts_cross_workspace_bytes(const tts_cross_config* cfg)
 {
     if (check(cfg) != TTS_OK) return 0;
-    return cross_parts_bytes();
+    return layout_of().total;
 }
 
 extern "C" int tts_cross_create(const tts_cross_config* cfg, void* dev_arena, size_t arena_bytes, void* hip_stream, tts_cross** out)
@@ -46,12 +58,18 @@ extern "C" int tts_cross_create(const tts_cross_config* cfg, void* dev_arena, si
     int rc = check(cfg);
     if (rc) return rc;
     int device = 0, n_cu = 0;
-    if ((rc = check_arena(dev_arena, arena_bytes, cross_parts_bytes(), &device))) return rc;
+    const Layout lay = layout_of();
+    if ((rc = check_arena(dev_arena, arena_bytes, lay.total, &device))) return rc;
+    OnDevice on(device);
+    HIP_TRY(on.err);
+    HIP_TRY(allow_cross());
+    HIP_TRY(fill_now((char*)dev_arena + lay.zeros, 0, 256));
     HIP_TRY(hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, device));
     tts_cross* p = new (std::nothrow) tts_cross();
     if (!p) return fail(TTS_E_INVAL, "out of host memory");
     p->cfg = *cfg;
-    p->parts = (float*)dev_arena;
+    p->parts = (float*)((char*)dev_arena + lay.parts);
+    p->zeros = (char*)dev_arena + lay.zeros;
     p->stream = (hipStream_t)hip_stream;
     p->device = device;
     p->n_cu = n_cu;
@@ -90,20 +108,26 @@ extern "C" int tts_cross_run(tts_cross* p, const tts_cross_batch* b, const tts_c
     a.keep = t->keep;
     a.lse = t->lse;
     a.parts = p->parts;
+    a.zeros = p->zeros;
     a.q_stride = stride[0]; a.k_stride = stride[1]; a.v_stride = stride[2]; a.out_stride = stride[3];
     a.scale = (t->scale > 0 ? t->scale : 1.0f / sqrtf((float)p->cfg.head_dim)) * 1.4426950408889634f;
     a.n_heads = p->cfg.n_heads; a.n_kv_heads = p->cfg.n_kv_heads; a.head_dim = p->cfg.head_dim;
     OnDevice on(p->device);
     HIP_TRY(on.err);
-    int q_row = 0;
-    for (int i = 0; i < b->n;) {
+    // two launches' worth: requests of few rows, and of many
+    const int group = p->cfg.n_heads / p->cfg.n_kv_heads;
+    const bool bf16 = p->cfg.dtype == TTS_DTYPE_BF16;
+    for (int many = 0; many < (bf16 ? 2 : 1); ++many) {
+        int q_row = 0;
         a.n = 0;
-        for (; i < b->n && a.n < CROSS_BATCH; ++i) {
-            if (!b->q_len[i]) continue;
-            a.req[a.n++] = CrossReq{b->mem_row[i], b->mem_len[i], q_row, b->q_len[i], 0};
+        for (int i = 0; i < b->n; ++i) {
+            if (b->q_len[i] && (bf16 && (long long)b->q_len[i] * group >= CROSS_MANY_ROWS) == many) a.req[a.n++] = CrossReq{b->mem_row[i], b->mem_len[i], q_row, b->q_len[i], 0};
             q_row += b->q_len[i];
+            if (a.n == CROSS_BATCH || (a.n && i + 1 == b->n)) {
+                HIP_TRY(many ? launch_cross_many(a, p->n_cu, p->stream) : launch_cross_few(a, bf16, p->stream));
+                a.n = 0;
+            }
         }
-        if (a.n) HIP_TRY(launch_cross(a, p->cfg.dtype == TTS_DTYPE_BF16, p->n_cu, p->stream));
     }
     return TTS_OK;
 }

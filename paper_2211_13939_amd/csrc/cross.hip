@@ -299,7 +299,229 @@ template <typename T, int D> __global__ __launch_bounds__(256) void k_cross_join
     });
 }
 
-template <typename T, int D, bool FULL> void go(const CrossArgs& a, int n_cu, hipStream_t s)
+// Many rows, two bytes: 32 * NW rows of a request and a key head, 32 a wave, over the memory in tiles of 64 keys that all waves read from LDS while
+// the next R - 1 are on their way there, 16 bytes a lane straight from memory; one barrier a tile.
+//
+// Scores are transposed as above, of 32 keys and 32 rows an instruction: lane l holds row l % 32 and of each 16 keys 4 h .. 4 h + 3 and 8 + 4 h .. + 3
+// (h = l / 32), which are eight of the second product's operand.  Its other operand, values with the keys along a lane, comes by LDS's transposing
+// reads.  Keys' 16-byte pieces and values' 64-byte ones change places from row to row, so that reads down a column find all banks.
+// Positions that are hidden or not there are loaded from zeros.  The sums are rescaled when a row's maximum has grown by more than 2^8: weights are at most
+// that large until then, and their quotient is the same.
+constexpr int KEYS = 64;
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+template <int D, int NW, int R> struct ManyRows {
+    static constexpr int ROW = 2 * D, PART = KEYS * ROW, SLOT = 2 * PART, LOADS = PART / 1024 / NW, LDS = R * SLOT + 2 * KEYS * 8;
+    static_assert(LOADS * 1024 * NW == PART, "shares of the waves");
+};
+// All but the last N loads of every wave are there, and all waves have read what they needed.
+template <int N> __device__ __forceinline__ void arrived()
+{
+    static_assert(N < 64, "the counter has six bits");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+// (written out as in linear8.hip: no registers to come back to, m0 has no other user)
+__device__ __forceinline__ void to_lds(const char* from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+
+template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW, 2) void k_cross_many(CrossArgs p)
+{
+    using M = ManyRows<D, NW, R>;
+    constexpr int ROW = M::ROW, ND = D / 32, NK = D / 16;
+    extern __shared__ __align__(16) char lds[];
+    uint64_t* masks = reinterpret_cast<uint64_t*>(lds + R * M::SLOT);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+    // Which tile: an XCD has a run of them, so that its L2 holds the memory that they share
+    const int xcd = blockIdx.x & 7, id = p.start[xcd] + (blockIdx.x >> 3);
+    if (id >= p.start[xcd + 1]) return;
+    const uint64_t before0 = __ballot(lane < p.n && p.req[min(lane, p.n - 1)].first <= id), before1 = __ballot(64 + lane < p.n && p.req[min(64 + lane, p.n - 1)].first <= id);
+    const CrossReq r = p.req[__popcll(before0) + __popcll(before1) - 1];
+    const int group = p.n_heads / p.n_kv_heads, rows = r.q_len * group, tiles = (rows + 32 * NW - 1) / (32 * NW);
+    const int kv = (id - r.first) / tiles, row = ((id - r.first) % tiles * NW + wave) * 32 + c, row_there = min(row, rows - 1);
+    const long long q_row = (long long)r.q_row + row_there / group;
+    const int head = kv * group + row_there % group;
+    uint4 q[NK];
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+        const int d = 16 * k + 8 * h;
+        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(p.q) + q_row * p.q_stride + head * p.head_dim + (d < p.head_dim ? d : 0));
+        q[k] = d < p.head_dim ? x : make_uint4(0, 0, 0, 0);
+    }
+    const int n_tiles = (r.mem_len + KEYS - 1) / KEYS;
+    const long long k_row = 2 * p.k_stride, v_row = 2 * p.v_stride;
+    // this wave's share of a tile: the row and piece that lie where the lane's 16 bytes go
+    const char *k_from[M::LOADS], *v_from[M::LOADS];
+    int from_row[M::LOADS];
+    bool k_there[M::LOADS], v_there[M::LOADS];
+#pragma unroll
+    for (int i = 0; i < M::LOADS; ++i) {
+        const int at = (wave + i * NW) * 1024 + lane * 16, at_row = at / ROW, piece = at % ROW / 16;
+        const int k_piece = piece ^ (at_row & (D / 8 - 1)), v_piece = piece ^ (D == 128 ? at_row & 3 : at_row >> 1 & 1) << 2;
+        from_row[i] = at_row;
+        k_there[i] = 8 * k_piece < p.head_dim;
+        v_there[i] = 8 * v_piece < p.head_dim;
+        k_from[i] = static_cast<const char*>(p.k) + (r.mem_row + at_row) * k_row + 2 * kv * p.head_dim + 16 * k_piece;
+        v_from[i] = static_cast<const char*>(p.v) + (r.mem_row + at_row) * v_row + 2 * kv * p.head_dim + 16 * v_piece;
+    }
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds;
+    // which of a tile's keys there are; with a mask, of 64 tiles at a time
+    auto there = [&](int tile) -> uint64_t {
+        if constexpr (MASK) {
+            const uint64_t m = masks[tile % (2 * KEYS)];
+            const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)m), high = __builtin_amdgcn_readfirstlane((uint32_t)(m >> 32));
+            return (uint64_t)high << 32 | low;
+        }
+        const int left = r.mem_len - tile * KEYS;
+        return left >= KEYS ? ~0ull : (1ull << left) - 1;
+    };
+    auto look = [&](int first) {
+        if constexpr (MASK)
+            for (int t = first + wave; t < first + KEYS && t < n_tiles; t += NW) {
+                const int key = t * KEYS + lane;
+                const uint64_t m = __ballot(key < r.mem_len && p.keep[r.mem_row + min(key, r.mem_len - 1)] != 0);
+                if (lane == 0) masks[t % (2 * KEYS)] = m;
+            }
+    };
+    auto bring = [&](int tile, int slot) {
+        const uint64_t m = there(tile);
+#pragma unroll
+        for (int i = 0; i < M::LOADS; ++i) {
+            const bool in = m >> from_row[i] & 1;
+            const char* k = k_from[i] + tile * (KEYS * k_row);
+            const char* v = v_from[i] + tile * (KEYS * v_row);
+            to_lds(in && k_there[i] ? k : static_cast<const char*>(p.zeros), lds_at + slot * M::SLOT + (wave + i * NW) * 1024);
+            to_lds(in && v_there[i] ? v : static_cast<const char*>(p.zeros), lds_at + slot * M::SLOT + M::PART + (wave + i * NW) * 1024);
+        }
+    };
+    floatx16 o[ND] = {};
+    float m = -__builtin_inff(), l = 0;
+    if (MASK) {
+        look(0);
+        __syncthreads();
+    }
+    for (int i = 0; i < R - 1 && i < n_tiles; ++i) bring(i, i);
+    for (int tile = 0, slot = 0, free = R - 1; tile < n_tiles; ++tile) {
+        // (the tiles behind this one that are on their way: R - 2 but at the end)
+        if (tile + R - 2 < n_tiles) arrived<(R - 2) * 2 * M::LOADS>();
+        else arrived<0>();
+        if (MASK && tile % KEYS == 0 && tile + KEYS < n_tiles) {
+            look(tile + KEYS);
+            __syncthreads();
+        }
+        if (tile + R - 1 < n_tiles) bring(tile + R - 1, free);
+        const uint64_t mask = there(tile);
+        if (mask != 0) {
+            const char* kt = lds + slot * M::SLOT + c * ROW;
+            floatx16 s[2] = {};
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                const char* at = kt + 16 * ((2 * k + h) ^ (c & (D / 8 - 1)));
+                const bf16x8 b = __builtin_bit_cast(bf16x8, q[k]);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(at + t * 32 * ROW), b, s[t], 0, 0, 0);
+            }
+            if (mask != ~0ull) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const uint32_t bits = (uint32_t)(mask >> (32 * t)) >> (4 * h);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[t][i] = bits >> (8 * (i / 4) + (i & 3)) & 1 ? s[t][i] : -__builtin_inff();
+                }
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * p.scale;
+            if (__any(top > m + 8.f)) {
+                top = fmaxf(m, top);
+                const float by = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.f : top));
+                m = top;
+                l *= by;
+#pragma unroll
+                for (int d = 0; d < ND; ++d) o[d] *= by;
+            }
+            const float base = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                s[i / 16][i % 16] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 16][i % 16], p.scale, -base));
+                l += s[i / 16][i % 16];
+            }
+            const char* vt = lds + slot * M::SLOT + M::PART + (4 * h + (lane >> 2 & 3)) * ROW + 32 * (lane >> 4 & 1) + 8 * (lane & 3);
+            const int turn = D == 128 ? lane >> 2 & 3 : lane >> 3 & 1;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                uint4 w;
+                const int i = 8 * (k & 1);
+                w.x = pack_bf16x2(s[k / 2][i], s[k / 2][i + 1]);
+                w.y = pack_bf16x2(s[k / 2][i + 2], s[k / 2][i + 3]);
+                w.z = pack_bf16x2(s[k / 2][i + 4], s[k / 2][i + 5]);
+                w.w = pack_bf16x2(s[k / 2][i + 6], s[k / 2][i + 7]);
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    using Four = __attribute__((address_space(3))) shortx4*;
+                    const char* at = vt + 16 * k * ROW + 64 * (d ^ turn);
+                    const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(at + 8 * ROW));
+                    const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, w), o[d], 0, 0, 0);
+                }
+            }
+        }
+        free = slot;                                     // (the slot that the tile before this one was in)
+        slot = slot + 1 == R ? 0 : slot + 1;
+    }
+    const auto sums = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(sums[0]) + __uint_as_float(sums[1]);
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    bf16_t* out = static_cast<bf16_t*>(p.out) + q_row * p.out_stride + head * p.head_dim;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 8) {
+            // columns 8 h' .. + 7 of each 16: the lanes that share a row exchange halves
+            const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[d][i] * inv, o[d][i + 1] * inv), pack_bf16x2(o[d][i + 4] * inv, o[d][i + 5] * inv), false, false);
+            const auto y = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[d][i + 2] * inv, o[d][i + 3] * inv), pack_bf16x2(o[d][i + 6] * inv, o[d][i + 7] * inv), false, false);
+            const int column = 32 * d + 2 * i + 8 * h;
+            if (row < rows && column < p.head_dim) *reinterpret_cast<uint4*>(out + column) = make_uint4(x[0], y[0], x[1], y[1]);
+        }
+    if (p.lse && row < rows && h == 0)
+        p.lse[q_row * p.n_heads + head] = l == 0.f ? -__builtin_inff() : ((m == -__builtin_inff() ? 0.f : m) + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <int D, int NW, int R> hipError_t allow()
+{
+    const auto a = k_cross_many<D, NW, R, false>, b = k_cross_many<D, NW, R, true>;
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(a), hipFuncAttributeMaxDynamicSharedMemorySize, ManyRows<D, NW, R>::LDS);
+    return e == hipSuccess ? hipFuncSetAttribute(reinterpret_cast<const void*>(b), hipFuncAttributeMaxDynamicSharedMemorySize, ManyRows<D, NW, R>::LDS) : e;
+}
+
+template <int D, int NW, int R> void go_many(CrossArgs& a, hipStream_t s)
+{
+    // shares of the XCDs: equal in keys that their tiles go over (and a tile's own cost, some 64 keys')
+    const int group = a.n_heads / a.n_kv_heads;
+    auto tiles_of = [&](const CrossReq& r) { return (int)(((long long)r.q_len * group + 32 * NW - 1) / (32 * NW)) * a.n_kv_heads; };
+    double work = 0, done = 0;
+    int tiles = 0, most = 0;
+    for (int i = 0; i < a.n; ++i) work += (double)tiles_of(a.req[i]) * (a.req[i].mem_len + KEYS);
+    int x = 1;
+    a.start[0] = 0;
+    for (int i = 0; i < a.n; ++i) {
+        a.req[i].first = tiles;
+        const int mine = tiles_of(a.req[i]), each = a.req[i].mem_len + KEYS;
+        for (; x < 8 && done + (double)mine * each >= work * x / 8; ++x) a.start[x] = std::min(tiles + mine, std::max(a.start[x - 1], tiles + (int)((work * x / 8 - done) / each + 0.5)));
+        tiles += mine;
+        done += (double)mine * each;
+    }
+    for (; x <= 8; ++x) a.start[x] = tiles;
+    for (int i = 0; i < 8; ++i) most = std::max(most, a.start[i + 1] - a.start[i]);
+    const auto kernel = a.keep ? k_cross_many<D, NW, R, true> : k_cross_many<D, NW, R, false>;
+    constexpr int LDS = ManyRows<D, NW, R>::LDS;
+    hipLaunchKernelGGL(kernel, dim3(8 * most), dim3(64 * NW), LDS, s, a);
+}
+
+template <typename T, int D, bool FULL> void go_few(const CrossArgs& a, hipStream_t s)
 {
     int tiles = 0, longest = 0;
     const int group = a.n_heads / a.n_kv_heads;
@@ -319,13 +541,31 @@ template <typename T, int D, bool FULL> void go(const CrossArgs& a, int n_cu, hi
 
 size_t cross_parts_bytes() { return (size_t)MAX_PARTS * part_floats(128) * 4; }
 
-hipError_t launch_cross(CrossArgs& a, bool bf16, int n_cu, hipStream_t s)
+hipError_t allow_cross()
+{
+    hipError_t e = allow<64, 4, 3>();
+    if (e == hipSuccess) e = allow<64, 8, 3>();
+    if (e == hipSuccess) e = allow<128, 4, 2>();
+    if (e == hipSuccess) e = allow<128, 8, 3>();
+    return e;
+}
+
+hipError_t launch_cross_few(const CrossArgs& a, bool bf16, hipStream_t s)
 {
     const bool wide = a.head_dim > 64, full = a.head_dim % 64 == 0;
-    if (bf16 && wide) full ? go<bf16_t, 128, true>(a, n_cu, s) : go<bf16_t, 128, false>(a, n_cu, s);
-    else if (bf16) full ? go<bf16_t, 64, true>(a, n_cu, s) : go<bf16_t, 64, false>(a, n_cu, s);
-    else if (wide) full ? go<float, 128, true>(a, n_cu, s) : go<float, 128, false>(a, n_cu, s);
-    else full ? go<float, 64, true>(a, n_cu, s) : go<float, 64, false>(a, n_cu, s);
+    if (bf16 && wide) full ? go_few<bf16_t, 128, true>(a, s) : go_few<bf16_t, 128, false>(a, s);
+    else if (bf16) full ? go_few<bf16_t, 64, true>(a, s) : go_few<bf16_t, 64, false>(a, s);
+    else if (wide) full ? go_few<float, 128, true>(a, s) : go_few<float, 128, false>(a, s);
+    else full ? go_few<float, 64, true>(a, s) : go_few<float, 64, false>(a, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_cross_many(CrossArgs& a, int n_cu, hipStream_t s)
+{
+    long long large = 0;
+    for (int i = 0; i < a.n; ++i) large += ((long long)a.req[i].q_len * (a.n_heads / a.n_kv_heads) + 255) / 256 * a.n_kv_heads;
+    if (a.head_dim > 64) large >= n_cu ? go_many<128, 8, 3>(a, s) : go_many<128, 4, 2>(a, s);
+    else large >= n_cu ? go_many<64, 8, 3>(a, s) : go_many<64, 4, 3>(a, s);
     return hipGetLastError();
 }
 

@@ -40,20 +40,28 @@ hipError_t launch_linear8(const Linear8Args& a, bool y_bf16, int n_cu, hipStream
 constexpr int CROSS_BATCH = 128;         // requests of a launch
 struct CrossReq {
     long long mem_row;
-    int mem_len, q_row, q_len, pad;
+    int mem_len, q_row, q_len;
+    int first;                           // of its row tiles, of all key heads, in the launch of many rows
 };
 struct CrossArgs {
     const void *q, *k, *v;
     void* out;
     const uint8_t* keep;
+    const void* zeros;                   // 16 bytes and more
     float *lse, *parts;
     long long q_stride, k_stride, v_stride, out_stride;        // elements
     float scale;                         // times log2(e)
     int n_heads, n_kv_heads, head_dim;
     int n;
+    int start[9];                        // of the row tiles that each XCD takes
     CrossReq req[CROSS_BATCH];
 };
 size_t cross_parts_bytes();
-hipError_t launch_cross(CrossArgs& a, bool bf16, int n_cu, hipStream_t s);
+hipError_t allow_cross();                // once on each device, before the first launch there
+// `few`: 16 rows a workgroup, both types; `many`: 128 or 256, two bytes alone (fills in what the launch's tiles are)
+hipError_t launch_cross_few(const CrossArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_cross_many(CrossArgs& a, int n_cu, hipStream_t s);
+// rows of a request and a key head from which it is the latter's
+constexpr int CROSS_MANY_ROWS = 33;
 
 }  // namespace tts

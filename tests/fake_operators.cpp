@@ -10,7 +10,7 @@
 
 namespace {
 std::string text;
-int current = 0, launches = 0, last_rows = 0, last_n = 0, first_q_row = 0, devices_seen = 0;
+int current = 0, launches = 0, last_rows = 0, last_n = 0, devices_seen = 0, requests_seen = 0, many_launches = 0;
 std::string failing;
 hipError_t call(const char* name) { return failing == name ? hipErrorUnknown : hipSuccess; }
 }  // namespace
@@ -41,24 +41,33 @@ hipError_t launch_linear8(const Linear8Args& a, bool, int, hipStream_t)
     return call("launch");
 }
 size_t cross_parts_bytes() { return 4096; }
-hipError_t launch_cross(CrossArgs& a, bool, int, hipStream_t)
+hipError_t allow_cross() { return call("allow"); }
+static hipError_t launched(const CrossArgs& a)
 {
-    if (!launches) first_q_row = a.req[0].q_row;
     ++launches;
     last_n = a.n;
     last_rows = a.req[a.n - 1].q_row + a.req[a.n - 1].q_len;
+    for (int i = 0; i < a.n; ++i) requests_seen += 1;
     return call("launch");
+}
+hipError_t launch_cross_few(const CrossArgs& a, bool, hipStream_t) { return launched(a); }
+hipError_t launch_cross_many(CrossArgs& a, int, hipStream_t)
+{
+    ++many_launches;
+    return launched(a);
 }
 }  // namespace tts
 
 extern "C" {
 const char* tts_last_error() { return text.c_str(); }
-void fake_reset() { text.clear(); failing.clear(); launches = last_rows = last_n = current = 0; }
+void fake_reset() { text.clear(); failing.clear(); launches = last_rows = last_n = current = requests_seen = many_launches = 0; }
 void fake_fail(const char* name) { failing = name; }
 void fake_device(int d) { current = d; }
 int fake_launches() { return launches; }
 int fake_rows() { return last_rows; }
 int fake_requests() { return last_n; }
+int fake_requests_seen() { return requests_seen; }
+int fake_many() { return many_launches; }
 int fake_current() { return current; }
 int fake_seen() { return devices_seen; }
 hipError_t hipGetDevice(int* d) { *d = current; return call("hipGetDevice"); }

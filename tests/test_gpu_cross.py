@@ -143,6 +143,28 @@ def test_long_memories_in_parts(n, heads, kv, d, mem, bf16):
     _run(torch, heads, kv, d, bf16, [2] * n, _packed(lens), lens, keep=keep, seed=mem + 1)
 
 
+@pytest.mark.parametrize("heads,kv,d,mem", [(2, 1, 64, 9000), (2, 2, 128, 8193)])
+def test_many_queries_over_long_hidden_memories(heads, kv, d, mem):
+    """More than the 4096 keys whose mask is looked at at once, whole stretches hidden."""
+    import torch
+    rng = np.random.default_rng(mem)
+    keep = rng.random(mem + 60) > 0.5
+    keep[:4200] = False
+    keep[5000:8190] = False
+    keep = torch.from_numpy(keep.astype(np.uint8)).to("cuda:0")
+    _run(torch, heads, kv, d, True, [150, 33], [0, mem], [mem, 60], keep=keep, seed=mem)
+    _run(torch, heads, kv, d, True, [150, 33], [0, mem], [mem, 60], seed=mem)
+
+
+@pytest.mark.parametrize("n,q,mem,d", [(20, 600, 70, 64), (40, 300, 130, 128)])
+def test_many_large_tiles(n, q, mem, d):
+    """Enough rows for 256 a workgroup, ragged, shares of the XCDs of different sizes."""
+    import torch
+    q_len = [(q * (i % 5 + 1)) // 3 for i in range(n)]
+    lens = [(mem * (i % 4)) for i in range(n)]
+    _run(torch, 8, 4, d, True, q_len, _packed(lens), lens, seed=n)
+
+
 @pytest.mark.parametrize("bf16", [False, True])
 def test_strides_a_shared_memory_and_a_scale(bf16):
     """Rows apart (as of a projection to keys and values together), two requests over one memory, overlapping memories, another scale."""

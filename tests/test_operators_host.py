@@ -225,6 +225,12 @@ def test_cross_refuses(lib):
     assert run(q_len=(0, 0, 0), q=None, out=None, k=None, v=None) == 0
     assert run(mem=(0, 0, 0), k=None, v=None) == 0
     assert run(q_len=[1] * 300, row=[0] * 300, mem=[1] * 300) == 0 and lib.fake_requests() == 300 % 128 and lib.fake_rows() == 300
+    # requests of many rows go by themselves (8 / 2 heads: 4 rows a query); every request once
+    lib.fake_reset()
+    assert run(q_len=[1, 500] * 70, row=[0] * 140, mem=[1] * 140) == 0
+    assert lib.fake_launches() == 2 and lib.fake_many() == 1 and lib.fake_requests_seen() == 140 and lib.fake_rows() == 70 * 501
+    lib.fake_reset()
+    assert run(q_len=[500] * 300, row=[0] * 300, mem=[1] * 300) == 0 and lib.fake_launches() == lib.fake_many() == 3 and lib.fake_requests_seen() == 300
     assert run(scale=0.5) == 0 and run(k_stride=1 << 24, q_stride=328, row=(1 << 40, 0, 0)) == 0
     for change in (dict(n=0), dict(n=-1), dict(null="q_len"), dict(null="mem_row"), dict(null="mem_len"), dict(q_len=(-1, 0, 0)), dict(q_len=((1 << 24) + 1, 0, 0)), dict(mem=(-1, 0, 0)),
                    dict(mem=((1 << 24) + 1, 0, 0)), dict(row=(-1, 0, 0)), dict(row=((1 << 40) + 1, 0, 0)), dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(q_stride=319), dict(q_stride=321),
