@@ -819,7 +819,10 @@ class _Operator:
         self._torch = torch
         self.cfg = cfg
         d = torch.device(device)
-        self.device = torch.device(d.type, torch.cuda.current_device() if d.index is None else d.index)
+        if d.type != "cuda":
+            raise ValueError(f"{device}: a GPU is wanted")
+        self._index = torch.cuda.current_device() if d.index is None else d.index
+        self.device = torch.device("cuda", self._index)
         nbytes = int(getattr(lib(), f"tts_{self._name}_workspace_bytes")(C.byref(cfg)))
         if nbytes == 0:
             raise TtsError(TTS_E_INVAL, lib().tts_last_error().decode("utf-8", "replace"))
@@ -834,25 +837,27 @@ class _Operator:
     def _type(self, dtype: int):
         return self._torch.bfloat16 if dtype == DTYPE_BF16 else self._torch.float32
 
+    # (the checks of a call's tensors are half of what it costs the host: one function a tensor, cheapest questions)
     def _at(self, t, name, dtype, shape) -> int:
         """Address of a tensor of this device, type and shape whose elements lie back to back."""
-        self._like(t, name, dtype, shape)
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index:
+            self._refuse(t, name, dtype, shape)
         if not t.is_contiguous():
             raise ValueError(f"{name}: its elements have to lie back to back")
         return t.data_ptr()
 
     def _rows(self, t, name, dtype, shape):
         """(address, distance of the rows) of one whose rows may lie apart; 0: back to back."""
-        self._like(t, name, dtype, shape)
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index:
+            self._refuse(t, name, dtype, shape)
         if t.is_contiguous():
             return t.data_ptr(), 0
         if t.stride(0) <= 0 or not t[0].is_contiguous():
             raise ValueError(f"{name}: the elements of a row have to lie back to back")
         return t.data_ptr(), t.stride(0)
 
-    def _like(self, t, name, dtype, shape) -> None:
-        if t.device != self.device or t.dtype != dtype or t.shape != shape:
-            raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device} where {tuple(shape)} {dtype} on {self.device} is wanted")
+    def _refuse(self, t, name, dtype, shape):
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device} where {tuple(shape)} {dtype} on {self.device} is wanted")
 
     def close(self) -> None:
         if getattr(self, "_handle", None):
@@ -883,28 +888,30 @@ class Norm(_Operator):
         if g is not None and g.shape != (cfg.dim,):
             raise ValueError(f"gain: {g.shape} where ({cfg.dim},) is wanted")
         _check(lib().tts_norm_create(C.byref(cfg), None if g is None else g.ctypes.data_as(_fp), *where))
-        self._types = [self._type(t) for t in (cfg.x_dtype, cfg.res_dtype, cfg.res_dtype, cfg.y_dtype)]
+        self._types = [self._type(t) for t in (cfg.x_dtype, cfg.res_dtype, cfg.y_dtype)]
+        self._dim, self._widths, self._types8 = cfg.dim, (width8(cfg.dim), scale_columns(cfg.dim)), (self._torch.float8_e4m3fn, self._torch.float8_e8m0fnu)
 
     def run_device(self, x, res=None, total=None, y=None, y8=None, scales=None) -> None:
         """x, res, total, y: CUDA [rows, dim] of the configuration's types, rows any distance apart; y8: float8_e4m3fn [rows, width8(dim)],
         scales: float8_e8m0fnu [rows, scale_columns(dim)].  Those that are None are not there.  Queued on the stream."""
-        shape, t = x.shape, self._types
-        if len(shape) != 2 or shape[1] != self.cfg.dim:
-            raise ValueError(f"x: {tuple(shape)} where [rows, {self.cfg.dim}] is wanted")
+        shape, (x_type, res_type, y_type) = x.shape, self._types
+        if len(shape) != 2 or shape[1] != self._dim:
+            raise ValueError(f"x: {tuple(shape)} where [rows, {self._dim}] is wanted")
+        rows = shape[0]
         a = TtsNormRows()
-        a.rows = shape[0]
-        a.x, a.x_stride = self._rows(x, "x", t[0], shape)
+        a.rows = rows
+        a.x, a.x_stride = self._rows(x, "x", x_type, shape)
         if res is not None:
-            a.res, a.res_stride = self._rows(res, "res", t[1], shape)
+            a.res, a.res_stride = self._rows(res, "res", res_type, shape)
         if total is not None:
-            a.total, a.total_stride = self._rows(total, "total", t[2], shape)
+            a.total, a.total_stride = self._rows(total, "total", res_type, shape)
         if y is not None:
-            a.y, a.y_stride = self._rows(y, "y", t[3], shape)
+            a.y, a.y_stride = self._rows(y, "y", y_type, shape)
         if y8 is not None:
-            a.y8 = self._at(y8, "y8", self._torch.float8_e4m3fn, (shape[0], width8(shape[1])))
+            a.y8 = self._at(y8, "y8", self._types8[0], (rows, self._widths[0]))
         if scales is not None:
-            a.scales = self._at(scales, "scales", self._torch.float8_e8m0fnu, (shape[0], scale_columns(shape[1])))
-        rc = self._run(self._handle, C.byref(a))
+            a.scales = self._at(scales, "scales", self._types8[1], (rows, self._widths[1]))
+        rc = self._run(self._handle, a)
         if rc:
             _check(rc)
 
@@ -926,14 +933,15 @@ class Linear8(_Operator):
             raise ValueError(f"w: {w.shape}, bias: {None if b is None else b.shape} where {(cfg.out_dim, cfg.in_dim)} and {(cfg.out_dim,)} are wanted")
         _check(lib().tts_linear8_create(C.byref(cfg), w.ctypes.data_as(_fp), None if b is None else b.ctypes.data_as(_fp), *where))
         self._y_type = self._type(cfg.y_dtype)
+        self._widths, self._types8 = (width8(cfg.in_dim), scale_columns(cfg.in_dim), cfg.out_dim), (self._torch.float8_e4m3fn, self._torch.float8_e8m0fnu)
 
     def run_device(self, x8, scales, y) -> None:
         """x8: CUDA float8_e4m3fn [rows, width8(in_dim)], zeros past in_dim; scales: float8_e8m0fnu [rows, scale_columns(in_dim)]; y: [rows, out_dim],
         rows any distance apart.  Queued on the stream."""
-        rows, k = x8.shape[0], self.cfg.in_dim
-        at = self._at(x8, "x8", self._torch.float8_e4m3fn, (rows, width8(k)))
-        sx = self._at(scales, "scales", self._torch.float8_e8m0fnu, (rows, scale_columns(k)))
-        rc = self._run(self._handle, at, sx, rows, *self._rows(y, "y", self._y_type, (rows, self.cfg.out_dim)))
+        rows, (k, n_scales, n) = x8.shape[0], self._widths
+        at = self._at(x8, "x8", self._types8[0], (rows, k))
+        sx = self._at(scales, "scales", self._types8[1], (rows, n_scales))
+        rc = self._run(self._handle, at, sx, rows, *self._rows(y, "y", self._y_type, (rows, n)))
         if rc:
             _check(rc)
 
@@ -964,6 +972,7 @@ class CrossAttention(_Operator):
         where = self._setup(cfg, stream, device)
         _check(lib().tts_cross_create(C.byref(cfg), *where))
         self._dtype = self._type(cfg.dtype)
+        self._heads = (cfg.n_heads, cfg.n_kv_heads, cfg.head_dim)
 
     def batch(self, q_len, mem_row, mem_len) -> CrossBatch:
         """A batch's lengths, for any number of calls."""
@@ -972,9 +981,9 @@ class CrossAttention(_Operator):
     def run_device(self, batch: CrossBatch, q, k, v, out, keep=None, lse=None, scale: float = 0.0) -> None:
         """q, out: CUDA [queries, n_heads, head_dim]; k, v: [memory rows, n_kv_heads, head_dim], rows any multiple of 8 elements apart; keep: uint8
         [memory rows], 0 = hidden; lse: fp32 [queries, n_heads].  Queued on the stream; scale 0: 1 / sqrt(head_dim)."""
-        c, t = self.cfg, self._dtype
+        t, (heads, kv, d) = self._dtype, self._heads
         rows = k.shape[0]
-        of_q, of_k = (batch.queries, c.n_heads, c.head_dim), (rows, c.n_kv_heads, c.head_dim)
+        of_q, of_k = (batch.queries, heads, d), (rows, kv, d)
         if rows < batch.memory_rows:
             raise ValueError(f"k has {rows} rows, the batch's memories end at {batch.memory_rows}")
         a = TtsCrossTensors()
@@ -987,6 +996,6 @@ class CrossAttention(_Operator):
         if lse is not None:
             a.lse = self._at(lse, "lse", self._torch.float32, of_q[:2])
         a.scale = scale
-        rc = self._run(self._handle, C.byref(batch.c), C.byref(a))
+        rc = self._run(self._handle, batch.c, a)
         if rc:
             _check(rc)

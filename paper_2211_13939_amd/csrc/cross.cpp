@@ -103,7 +103,7 @@ extern "C" int tts_cross_run(tts_cross* p, const tts_cross_batch* b, const tts_c
         if (!aligned(arrays[i].at, 16)) return fail(TTS_E_INVAL, "%s must be 16-byte aligned", arrays[i].name);
     }
     if (!aligned(t->lse, 4)) return fail(TTS_E_INVAL, "lse must be 4-byte aligned");
-    CrossArgs a{};
+    CrossArgs a;                             // (4 KB; of the requests what is used is filled in)
     a.q = t->q; a.k = t->k; a.v = t->v; a.out = t->out;
     a.keep = t->keep;
     a.lse = t->lse;
@@ -117,14 +117,17 @@ extern "C" int tts_cross_run(tts_cross* p, const tts_cross_batch* b, const tts_c
     // two launches' worth: requests of few rows, and of many
     const int group = p->cfg.n_heads / p->cfg.n_kv_heads;
     const bool bf16 = p->cfg.dtype == TTS_DTYPE_BF16;
-    for (int many = 0; many < (bf16 ? 2 : 1); ++many) {
+    long long few_tiles = 0;
+    for (int i = 0; i < b->n; ++i) few_tiles += ((long long)b->q_len[i] * group + 15) / 16 * p->cfg.n_kv_heads;
+    const bool any_many = bf16 && cross_many(few_tiles, p->n_cu);
+    for (int many = 0; many < 1 + any_many; ++many) {
         int q_row = 0;
         a.n = 0;
         for (int i = 0; i < b->n; ++i) {
-            if (b->q_len[i] && (bf16 && (long long)b->q_len[i] * group >= CROSS_MANY_ROWS) == many) a.req[a.n++] = CrossReq{b->mem_row[i], b->mem_len[i], q_row, b->q_len[i], 0};
+            if (b->q_len[i] && (any_many && (long long)b->q_len[i] * group >= CROSS_MANY_ROWS) == many) a.req[a.n++] = CrossReq{b->mem_row[i], b->mem_len[i], q_row, b->q_len[i], 0};
             q_row += b->q_len[i];
             if (a.n == CROSS_BATCH || (a.n && i + 1 == b->n)) {
-                HIP_TRY(many ? launch_cross_many(a, p->n_cu, p->stream) : launch_cross_few(a, bf16, p->stream));
+                HIP_TRY(many ? launch_cross_many(a, p->n_cu, p->stream) : launch_cross_few(a, bf16, p->n_cu, p->stream));
                 a.n = 0;
             }
         }

@@ -15,7 +15,7 @@ namespace tts {
 namespace {
 
 constexpr int FEW_WAVES = 4;
-constexpr int MAX_PARTS = 1024, MAX_SPLITS = 64;     // parts of one launch, of one row tile
+constexpr int MAX_PARTS = 1024, MAX_SPLITS = 256;    // parts of one launch, of one row tile
 constexpr int part_floats(int d) { return 16 * (d + 2); }
 
 // of the four lanes that share l % 16
@@ -203,7 +203,7 @@ __device__ __forceinline__ void finish_row(const CrossArgs& p, const CrossReq& r
 }
 
 // A tile of 16 rows over a part of its request's memory; the waves take steps of keys in turn, the next one's on its way, and meet in LDS.
-template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(FEW_WAVES * 64) void k_cross_few(CrossArgs p, int splits)
+template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(FEW_WAVES * 64) void k_cross_few(CrossArgs p, int splits, int share)
 {
     using G = Geometry<T, D>;
     constexpr int NE = G::NE, PITCH = D + 4, STRIDE = FEW_WAVES * G::N;
@@ -214,8 +214,8 @@ template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(
     const int group = p.n_heads / p.n_kv_heads, rows = r.q_len * group;
     if (16 * tile >= rows) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, g = lane >> 4;
-    const int share = ((r.mem_len + splits - 1) / splits + G::N - 1) / G::N * G::N;
     const int begin = split * share, end = min(r.mem_len, begin + share);
+    if (split > 0 && begin >= r.mem_len) return;
     const int row = 16 * tile + (lane & 15);
     const T* q_at = static_cast<const T*>(p.q) + ((long long)r.q_row + min(row, rows - 1) / group) * p.q_stride + (kv * group + min(row, rows - 1) % group) * p.head_dim;
     uint4 q[G::NF];
@@ -287,16 +287,60 @@ template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(
     }
 }
 
-template <typename T, int D> __global__ __launch_bounds__(256) void k_cross_join(CrossArgs p, int splits)
+// A row from its parts: their maxima give each a weight, then groups of D / 4 threads take parts in turn, four columns a thread, and meet in LDS.
+constexpr int JOIN = 256;
+static_assert(MAX_SPLITS <= JOIN, "a thread for every part");
+template <typename T, int D> __global__ __launch_bounds__(JOIN) void k_cross_join(CrossArgs p, int splits, int share)
 {
-    constexpr int NE = D / 16;
+    constexpr int ACROSS = D / 4, GROUPS = JOIN / ACROSS;
+    __shared__ float s_w[JOIN], s_top[JOIN / 64], s_sum[JOIN / 64];
+    __shared__ float4 s_o[GROUPS][ACROSS];
     const CrossReq r = p.req[blockIdx.z];
-    const int kv = blockIdx.y, tile = blockIdx.x, in_tile = threadIdx.x / 16, chunk = threadIdx.x & 15;
-    const float* parts = p.parts + (((size_t)blockIdx.z * p.n_kv_heads + kv) * gridDim.x + tile) * splits * part_floats(D);
-    finish_row<T, D>(p, r, kv, 16 * tile + in_tile, chunk, splits, [&](int i, int what) -> const float* {
-        const float* part = parts + (size_t)i * part_floats(D);
-        return what == 2 ? part + in_tile * D + NE * chunk : part + 16 * D + 16 * what + in_tile;
-    });
+    const int kv = blockIdx.y, tile = blockIdx.x / 16, in_tile = blockIdx.x % 16, group = p.n_heads / p.n_kv_heads, row = 16 * tile + in_tile;
+    if (row >= r.q_len * group) return;
+    const int n_parts = max(1, (r.mem_len + share - 1) / share), wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+    const float* parts = p.parts + (((size_t)blockIdx.z * p.n_kv_heads + kv) * (gridDim.x / 16) + tile) * splits * part_floats(D);
+    const bool mine = (int)threadIdx.x < n_parts;
+    const float* ml = parts + (size_t)(mine ? threadIdx.x : 0) * part_floats(D) + 16 * D + in_tile;
+    const float m = mine ? ml[0] : -__builtin_inff(), l = mine ? ml[16] : 0.f;
+    const float top_here = wave_max(m);
+    if (lane == 0) s_top[wave] = top_here;
+    __syncthreads();
+    const float top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])), base = top == -__builtin_inff() ? 0.f : top;
+    const float by = __builtin_amdgcn_exp2f(m - base), sum_here = wave_sum(by * l);
+    s_w[threadIdx.x] = by;
+    if (lane == 0) s_sum[wave] = sum_here;
+    __syncthreads();
+    const float sum = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+    const int column = threadIdx.x % ACROSS;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float* from = parts + in_tile * D + 4 * column;
+#pragma unroll 4
+    for (int i = threadIdx.x / ACROSS; i < n_parts; i += GROUPS) {
+        const float4 x = *reinterpret_cast<const float4*>(from + (size_t)i * part_floats(D));
+        const float w = s_w[i];
+        o.x += w * x.x;
+        o.y += w * x.y;
+        o.z += w * x.z;
+        o.w += w * x.w;
+    }
+    s_o[threadIdx.x / ACROSS][column] = o;
+    __syncthreads();
+    if (threadIdx.x >= ACROSS) return;
+#pragma unroll
+    for (int i = 1; i < GROUPS; ++i) {
+        const float4 x = s_o[i][column];
+        o.x += x.x;
+        o.y += x.y;
+        o.z += x.z;
+        o.w += x.w;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    const float v[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+    const long long q_row = (long long)r.q_row + row / group;
+    const int head = kv * group + row % group;
+    if (4 * column < p.head_dim) store_columns<T, 4>(static_cast<T*>(p.out) + q_row * p.out_stride + head * p.head_dim + 4 * column, v);
+    if (p.lse && threadIdx.x == 0) p.lse[q_row * p.n_heads + head] = sum == 0.f ? -__builtin_inff() : (base + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 // Many rows, two bytes: 32 * NW rows of a request and a key head, 32 a wave, over the memory in tiles of 64 keys that all waves read from LDS while
@@ -326,7 +370,9 @@ __device__ __forceinline__ void to_lds(const char* from, uint32_t to)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
 }
 
-template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW, 2) void k_cross_many(CrossArgs p)
+// (128 registers where heads are narrow and tiles large: with 135 of them 3 waves in place of 4 share a SIMD, and 16 heads of 3000 x 3000 x 64 in eight requests
+// take 366 in place of 328 us)
+template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : NW == 8 ? 4 : 3) void k_cross_many(CrossArgs p)
 {
     using M = ManyRows<D, NW, R>;
     constexpr int ROW = M::ROW, ND = D / 32, NK = D / 16;
@@ -401,7 +447,11 @@ template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW,
         look(0);
         __syncthreads();
     }
-    for (int i = 0; i < R - 1 && i < n_tiles; ++i) bring(i, i);
+    if (n_tiles) bring(0, 0);
+    // The queries are here, with the first tile: waited for in the loop, they would be together with the tiles that are on their way.
+#pragma unroll
+    for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(q[k].x), "+v"(q[k].y), "+v"(q[k].z), "+v"(q[k].w));
+    for (int i = 1; i < R - 1 && i < n_tiles; ++i) bring(i, i);
     for (int tile = 0, slot = 0, free = R - 1; tile < n_tiles; ++tile) {
         // (the tiles behind this one that are on their way: R - 2 but at the end)
         if (tile + R - 2 < n_tiles) arrived<(R - 2) * 2 * M::LOADS>();
@@ -422,6 +472,14 @@ template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW,
 #pragma unroll
                 for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(at + t * 32 * ROW), b, s[t], 0, 0, 0);
             }
+            // reads two steps ahead of their products (left alone, the compiler puts each in front of its use)
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int k = 0; k < NK - 2; ++k) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
             if (mask != ~0ull) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
@@ -521,7 +579,7 @@ template <int D, int NW, int R> void go_many(CrossArgs& a, hipStream_t s)
     hipLaunchKernelGGL(kernel, dim3(8 * most), dim3(64 * NW), LDS, s, a);
 }
 
-template <typename T, int D, bool FULL> void go_few(const CrossArgs& a, hipStream_t s)
+template <typename T, int D, bool FULL> void go_few(const CrossArgs& a, int n_cu, hipStream_t s)
 {
     int tiles = 0, longest = 0;
     const int group = a.n_heads / a.n_kv_heads;
@@ -529,12 +587,23 @@ template <typename T, int D, bool FULL> void go_few(const CrossArgs& a, hipStrea
         tiles = std::max(tiles, (a.req[i].q_len * group + 15) / 16);
         longest = std::max(longest, a.req[i].mem_len);
     }
-    const long long wgs = (long long)tiles * a.n_kv_heads * a.n;
-    int splits = (int)std::min<long long>({MAX_PARTS / wgs, (long long)MAX_SPLITS, (long long)longest / 256});
-    if (splits < 2) splits = 1;
+    // A workgroup by itself takes its memory at 50 to 100 GB/s (some 0.6 us for a step of its four waves), the join's launch costs 3 us.  So a memory is split where
+    // workgroups are few and it is long, into parts of equal length, of all requests alike, so that a round of them ends together.  us, whole / split, 8 heads of 64,
+    // bf16, requests x keys: 1 x 500 5.7 / 7.1, 1 x 1000 8.3 / 7.1, 1 x 30000 - / 17.5, 8 x 1000 8.4 / 8.6, 8 x 4000 23.7 / 18.0, 16 x 4000 24.4 / 28.4, 16 x
+    // 16000 153 / 119, 32 x 16000 209 / 231; 4 x 27000, 8 heads of 128 that four share each, 339 / 88 (5.05 TB/s).
+    const long long wgs = (long long)tiles * a.n_kv_heads * a.n, bytes = (long long)longest * D * sizeof(T);
+    int splits = 1, share = std::max(longest, 1);
+    if ((wgs <= n_cu / 4 && bytes >= 128 << 10) || (wgs <= n_cu / 2 && bytes >= 1 << 20)) {
+        long long keys = 0;
+        for (int i = 0; i < a.n; ++i) keys += a.req[i].mem_len;
+        const long long most = std::min<long long>(MAX_PARTS / wgs, MAX_SPLITS), even = keys * tiles * a.n_kv_heads / MAX_PARTS;
+        share = (int)((std::max({even, (longest + most - 1) / most, 128LL}) + 31) / 32 * 32);
+        splits = (longest + share - 1) / share;
+        if (splits < 2) splits = 1, share = longest;
+    }
     const auto kernel = a.keep ? k_cross_few<T, D, FULL, true> : k_cross_few<T, D, FULL, false>;
-    hipLaunchKernelGGL(kernel, dim3(tiles * splits, a.n_kv_heads, a.n), dim3(FEW_WAVES * 64), 0, s, a, splits);
-    if (splits > 1) hipLaunchKernelGGL((k_cross_join<T, D>), dim3(tiles, a.n_kv_heads, a.n), dim3(256), 0, s, a, splits);
+    hipLaunchKernelGGL(kernel, dim3(tiles * splits, a.n_kv_heads, a.n), dim3(FEW_WAVES * 64), 0, s, a, splits, share);
+    if (splits > 1) hipLaunchKernelGGL((k_cross_join<T, D>), dim3(16 * tiles, a.n_kv_heads, a.n), dim3(JOIN), 0, s, a, splits, share);
 }
 
 }  // namespace
@@ -550,22 +619,30 @@ hipError_t allow_cross()
     return e;
 }
 
-hipError_t launch_cross_few(const CrossArgs& a, bool bf16, hipStream_t s)
+hipError_t launch_cross_few(const CrossArgs& a, bool bf16, int n_cu, hipStream_t s)
 {
     const bool wide = a.head_dim > 64, full = a.head_dim % 64 == 0;
-    if (bf16 && wide) full ? go_few<bf16_t, 128, true>(a, s) : go_few<bf16_t, 128, false>(a, s);
-    else if (bf16) full ? go_few<bf16_t, 64, true>(a, s) : go_few<bf16_t, 64, false>(a, s);
-    else if (wide) full ? go_few<float, 128, true>(a, s) : go_few<float, 128, false>(a, s);
-    else full ? go_few<float, 64, true>(a, s) : go_few<float, 64, false>(a, s);
+    if (bf16 && wide) full ? go_few<bf16_t, 128, true>(a, n_cu, s) : go_few<bf16_t, 128, false>(a, n_cu, s);
+    else if (bf16) full ? go_few<bf16_t, 64, true>(a, n_cu, s) : go_few<bf16_t, 64, false>(a, n_cu, s);
+    else if (wide) full ? go_few<float, 128, true>(a, n_cu, s) : go_few<float, 128, false>(a, n_cu, s);
+    else full ? go_few<float, 64, true>(a, n_cu, s) : go_few<float, 64, false>(a, n_cu, s);
     return hipGetLastError();
 }
 
 hipError_t launch_cross_many(CrossArgs& a, int n_cu, hipStream_t s)
 {
+    // 256 rows a workgroup where memories are long and it leaves some for most compute units, 128 otherwise.  us, 128 / 256: 8 requests of 3000 queries over
+    // 3000 keys, 16 heads of 64 356 / 325, 16 of 128 that share 4 620 / 560; one of 4000 over 4000 (252 workgroups) 143 / 134, of 1000 over 1000 24 / 31;
+    // 64 of 600 over 135 33 / 35.
     long long large = 0;
-    for (int i = 0; i < a.n; ++i) large += ((long long)a.req[i].q_len * (a.n_heads / a.n_kv_heads) + 255) / 256 * a.n_kv_heads;
-    if (a.head_dim > 64) large >= n_cu ? go_many<128, 8, 3>(a, s) : go_many<128, 4, 2>(a, s);
-    else large >= n_cu ? go_many<64, 8, 3>(a, s) : go_many<64, 4, 3>(a, s);
+    int longest = 0;
+    for (int i = 0; i < a.n; ++i) {
+        large += ((long long)a.req[i].q_len * (a.n_heads / a.n_kv_heads) + 255) / 256 * a.n_kv_heads;
+        longest = std::max(longest, a.req[i].mem_len);
+    }
+    const bool eight = longest >= 1024 && large >= n_cu - n_cu / 4;
+    if (a.head_dim > 64) eight ? go_many<128, 8, 3>(a, s) : go_many<128, 4, 2>(a, s);
+    else eight ? go_many<64, 8, 3>(a, s) : go_many<64, 4, 3>(a, s);
     return hipGetLastError();
 }
 

@@ -59,9 +59,12 @@ struct CrossArgs {
 size_t cross_parts_bytes();
 hipError_t allow_cross();                // once on each device, before the first launch there
 // `few`: 16 rows a workgroup, both types; `many`: 128 or 256, two bytes alone (fills in what the launch's tiles are)
-hipError_t launch_cross_few(const CrossArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_cross_few(const CrossArgs& a, bool bf16, int n_cu, hipStream_t s);
 hipError_t launch_cross_many(CrossArgs& a, int n_cu, hipStream_t s);
-// rows of a request and a key head from which it is the latter's
+// A request is the latter's from two of the former's row tiles up, if the call has two and a half of those for every compute unit.  us, few / many: 16
+// requests, 8 heads of 64, 135 keys: 64 queries each (512 tiles) 5.4 / 6.5, 96 (768) 6.9 / 7.0, 192 (1536) 11.7 / 7.4; one of 1000 over 1000 keys (504) 20.7 /
+// 19.4, with 16 heads of 128 that share 4 (1000) 41 / 24; 32 requests of 40 queries over 300, 8 heads that share one (640) 9.2 / 8.8.
 constexpr int CROSS_MANY_ROWS = 33;
+inline bool cross_many(long long few_tiles, int n_cu) { return 2 * few_tiles >= 5LL * n_cu; }
 
 }  // namespace tts
