@@ -9,6 +9,7 @@
 #include "mfma.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace tts {
 
@@ -430,24 +431,104 @@ template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW,
                 if (lane == 0) masks[t % (2 * KEYS)] = m;
             }
     };
-    auto bring = [&](int tile, int slot) {
+    // (keys that are hidden may hold anything, their scores are not looked at; values count even with weight 0)
+    auto bring_keys = [&](int tile, int slot) {
+#pragma unroll
+        for (int i = 0; i < M::LOADS; ++i) {
+            const bool in = tile * KEYS + from_row[i] < r.mem_len;
+            to_lds(in && k_there[i] ? k_from[i] + tile * (KEYS * k_row) : static_cast<const char*>(p.zeros), lds_at + slot * M::SLOT + (wave + i * NW) * 1024);
+        }
+    };
+    auto bring_values = [&](int tile, int slot) {
         const uint64_t m = there(tile);
 #pragma unroll
         for (int i = 0; i < M::LOADS; ++i) {
             const bool in = m >> from_row[i] & 1;
-            const char* k = k_from[i] + tile * (KEYS * k_row);
-            const char* v = v_from[i] + tile * (KEYS * v_row);
-            to_lds(in && k_there[i] ? k : static_cast<const char*>(p.zeros), lds_at + slot * M::SLOT + (wave + i * NW) * 1024);
-            to_lds(in && v_there[i] ? v : static_cast<const char*>(p.zeros), lds_at + slot * M::SLOT + M::PART + (wave + i * NW) * 1024);
+            to_lds(in && v_there[i] ? v_from[i] + tile * (KEYS * v_row) : static_cast<const char*>(p.zeros), lds_at + slot * M::SLOT + M::PART + (wave + i * NW) * 1024);
         }
+    };
+    auto bring = [&](int tile, int slot) {
+        bring_keys(tile, slot);
+        bring_values(tile, slot);
     };
     floatx16 o[ND] = {};
     float m = -__builtin_inff(), l = 0;
+    // a tile, or its first 32 keys where there are no others
+    auto take = [&](int slot, uint64_t mask, auto halves) {
+        constexpr int N = decltype(halves)::value;
+        const char* kt = lds + slot * M::SLOT + c * ROW;
+        floatx16 s[N] = {};
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+            const char* at = kt + 16 * ((2 * k + h) ^ (c & (D / 8 - 1)));
+            const bf16x8 b = __builtin_bit_cast(bf16x8, q[k]);
+#pragma unroll
+            for (int t = 0; t < N; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(at + t * 32 * ROW), b, s[t], 0, 0, 0);
+        }
+        // reads two steps ahead of their products (left alone, the compiler puts each in front of its use)
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * N, 0);
+#pragma unroll
+        for (int k = 0; k < NK - 2; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, N, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, N, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 2 * N, 0);
+        if (mask != (N == 2 ? ~0ull : 0xFFFFFFFFull)) {
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                const uint32_t bits = (uint32_t)(mask >> (32 * t)) >> (4 * h);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t in = __builtin_amdgcn_sbfe((int)bits, 8 * (i / 4) + (i & 3), 1);        // all bits or none
+                    s[t][i] = __uint_as_float((__float_as_uint(s[t][i]) & in) | (0xFF800000u & ~in));
+                }
+            }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 16 * N; ++i) top = fmaxf(top, s[i / 16][i % 16]);
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * p.scale;
+        if (__any(top > m + 8.f)) {
+            top = fmaxf(m, top);
+            const float by = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.f : top));
+            m = top;
+            l *= by;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) o[d] *= by;
+        }
+        const float base = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+        for (int i = 0; i < 16 * N; ++i) {
+            s[i / 16][i % 16] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 16][i % 16], p.scale, -base));
+            l += s[i / 16][i % 16];
+        }
+        const char* vt = lds + slot * M::SLOT + M::PART + (4 * h + (lane >> 2 & 3)) * ROW + 32 * (lane >> 4 & 1) + 8 * (lane & 3);
+        const int turn = D == 128 ? lane >> 2 & 3 : lane >> 3 & 1;
+#pragma unroll
+        for (int k = 0; k < 2 * N; ++k) {
+            uint4 w;
+            const int i = 8 * (k & 1);
+            w.x = pack_bf16x2(s[k / 2][i], s[k / 2][i + 1]);
+            w.y = pack_bf16x2(s[k / 2][i + 2], s[k / 2][i + 3]);
+            w.z = pack_bf16x2(s[k / 2][i + 4], s[k / 2][i + 5]);
+            w.w = pack_bf16x2(s[k / 2][i + 6], s[k / 2][i + 7]);
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                using Four = __attribute__((address_space(3))) shortx4*;
+                const char* at = vt + 16 * k * ROW + 64 * (d ^ turn);
+                const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(at + 8 * ROW));
+                const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, w), o[d], 0, 0, 0);
+            }
+        }
+    };
+    if (n_tiles) bring_keys(0, 0);
     if (MASK) {
         look(0);
         __syncthreads();
     }
-    if (n_tiles) bring(0, 0);
+    if (n_tiles) bring_values(0, 0);
     // The queries are here, with the first tile: waited for in the loop, they would be together with the tiles that are on their way.
 #pragma unroll
     for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(q[k].x), "+v"(q[k].y), "+v"(q[k].z), "+v"(q[k].w));
@@ -462,71 +543,9 @@ template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW,
         }
         if (tile + R - 1 < n_tiles) bring(tile + R - 1, free);
         const uint64_t mask = there(tile);
-        if (mask != 0) {
-            const char* kt = lds + slot * M::SLOT + c * ROW;
-            floatx16 s[2] = {};
-#pragma unroll
-            for (int k = 0; k < NK; ++k) {
-                const char* at = kt + 16 * ((2 * k + h) ^ (c & (D / 8 - 1)));
-                const bf16x8 b = __builtin_bit_cast(bf16x8, q[k]);
-#pragma unroll
-                for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(at + t * 32 * ROW), b, s[t], 0, 0, 0);
-            }
-            // reads two steps ahead of their products (left alone, the compiler puts each in front of its use)
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-            for (int k = 0; k < NK - 2; ++k) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-            if (mask != ~0ull) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const uint32_t bits = (uint32_t)(mask >> (32 * t)) >> (4 * h);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[t][i] = bits >> (8 * (i / 4) + (i & 3)) & 1 ? s[t][i] : -__builtin_inff();
-                }
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
-            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-            top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * p.scale;
-            if (__any(top > m + 8.f)) {
-                top = fmaxf(m, top);
-                const float by = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.f : top));
-                m = top;
-                l *= by;
-#pragma unroll
-                for (int d = 0; d < ND; ++d) o[d] *= by;
-            }
-            const float base = m == -__builtin_inff() ? 0.f : m;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                s[i / 16][i % 16] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 16][i % 16], p.scale, -base));
-                l += s[i / 16][i % 16];
-            }
-            const char* vt = lds + slot * M::SLOT + M::PART + (4 * h + (lane >> 2 & 3)) * ROW + 32 * (lane >> 4 & 1) + 8 * (lane & 3);
-            const int turn = D == 128 ? lane >> 2 & 3 : lane >> 3 & 1;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint4 w;
-                const int i = 8 * (k & 1);
-                w.x = pack_bf16x2(s[k / 2][i], s[k / 2][i + 1]);
-                w.y = pack_bf16x2(s[k / 2][i + 2], s[k / 2][i + 3]);
-                w.z = pack_bf16x2(s[k / 2][i + 4], s[k / 2][i + 5]);
-                w.w = pack_bf16x2(s[k / 2][i + 6], s[k / 2][i + 7]);
-#pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    using Four = __attribute__((address_space(3))) shortx4*;
-                    const char* at = vt + 16 * k * ROW + 64 * (d ^ turn);
-                    const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(at + 8 * ROW));
-                    const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, w), o[d], 0, 0, 0);
-                }
-            }
-        }
+        // (a form of its own for half a tile costs registers: only where they are to spare, and memories short)
+        if (mask >> 32 != 0 || (mask != 0 && !(D == 64 && NW == 4))) take(slot, mask, std::integral_constant<int, 2>());
+        else if (D == 64 && NW == 4 && mask != 0) take(slot, mask, std::integral_constant<int, 1>());
         free = slot;                                     // (the slot that the tile before this one was in)
         slot = slot + 1 == R ? 0 : slot + 1;
     }
@@ -557,17 +576,19 @@ template <int D, int NW, int R> hipError_t allow()
 
 template <int D, int NW, int R> void go_many(CrossArgs& a, hipStream_t s)
 {
-    // shares of the XCDs: equal in keys that their tiles go over (and a tile's own cost, some 64 keys')
+    // shares of the XCDs: equal in keys that their tiles go over, and a tile's own cost, some 160 keys' (16 requests of 600 queries, 8 heads of 64, over 64 keys 7.5
+    // us, over 250 12.8, of which 2 are the launch's)
+    constexpr int OWN = 160;
     const int group = a.n_heads / a.n_kv_heads;
     auto tiles_of = [&](const CrossReq& r) { return (int)(((long long)r.q_len * group + 32 * NW - 1) / (32 * NW)) * a.n_kv_heads; };
     double work = 0, done = 0;
     int tiles = 0, most = 0;
-    for (int i = 0; i < a.n; ++i) work += (double)tiles_of(a.req[i]) * (a.req[i].mem_len + KEYS);
+    for (int i = 0; i < a.n; ++i) work += (double)tiles_of(a.req[i]) * (a.req[i].mem_len + OWN);
     int x = 1;
     a.start[0] = 0;
     for (int i = 0; i < a.n; ++i) {
         a.req[i].first = tiles;
-        const int mine = tiles_of(a.req[i]), each = a.req[i].mem_len + KEYS;
+        const int mine = tiles_of(a.req[i]), each = a.req[i].mem_len + OWN;
         for (; x < 8 && done + (double)mine * each >= work * x / 8; ++x) a.start[x] = std::min(tiles + mine, std::max(a.start[x - 1], tiles + (int)((work * x / 8 - done) / each + 0.5)));
         tiles += mine;
         done += (double)mine * each;
