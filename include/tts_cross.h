@@ -81,6 +81,7 @@ int tts_cross_create(const tts_cross_config *cfg, void *dev_arena, size_t arena_
  */
 int tts_cross_run(tts_cross *att, const tts_cross_batch *batch, const tts_cross_tensors *tensors);
 
+/* Does not wait: the arena stays the caller's to keep until the calls that were queued, and graphs that hold any, have run. */
 void tts_cross_destroy(tts_cross *att);
 
 #ifdef __cplusplus

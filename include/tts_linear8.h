@@ -58,6 +58,7 @@ int tts_linear8_create(const tts_linear8_config *cfg, const float *w, const floa
  */
 int tts_linear8_run(tts_linear8 *lin, const void *x8, const void *scales, int rows, void *y, long long y_stride);
 
+/* Does not wait: the arena stays the caller's to keep until the calls that were queued, and graphs that hold any, have run. */
 void tts_linear8_destroy(tts_linear8 *lin);
 
 #ifdef __cplusplus

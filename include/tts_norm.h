@@ -81,6 +81,7 @@ int tts_norm_create(const tts_norm_config *cfg, const float *gain, void *dev_are
  */
 int tts_norm_run(tts_norm *norm, const tts_norm_rows *rows);
 
+/* Does not wait: the arena stays the caller's to keep until the calls that were queued, and graphs that hold any, have run. */
 void tts_norm_destroy(tts_norm *norm);
 
 #ifdef __cplusplus

@@ -830,6 +830,7 @@ class _Operator:
             self.arena = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
             self.stream = stream if stream is not None else torch.cuda.Stream(device=self.device)
             torch.cuda.current_stream().synchronize()      # (the arena's memory may have been in use on this stream)
+            self.arena.record_stream(self.stream)          # (an object may go while its last calls are under way: its memory is not handed on before they end)
         self._handle = C.c_void_p()
         self._run = getattr(lib(), f"tts_{self._name}_run")
         return C.c_void_p(self.arena.data_ptr()), nbytes, C.c_void_p(self.stream.cuda_stream), C.byref(self._handle)

