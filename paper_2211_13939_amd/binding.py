@@ -838,27 +838,21 @@ class _Operator:
     def _type(self, dtype: int):
         return self._torch.bfloat16 if dtype == DTYPE_BF16 else self._torch.float32
 
-    # (the checks of a call's tensors are half of what it costs the host: one function a tensor, cheapest questions)
-    def _at(self, t, name, dtype, shape) -> int:
-        """Address of a tensor of this device, type and shape whose elements lie back to back."""
-        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index:
-            self._refuse(t, name, dtype, shape)
-        if not t.is_contiguous():
-            raise ValueError(f"{name}: its elements have to lie back to back")
+    # (the checks of a call's tensors are half of what it costs the host: one function a tensor, cheapest questions first)
+    def _at(self, t, name, dtype, count) -> int:
+        """Address of a tensor of this device and type with so many elements, back to back."""
+        if t.dtype is not dtype or t.get_device() != self._index or t.numel() != count or not t.is_contiguous():
+            raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device} where {count} elements, back to back, of {dtype} on {self.device} are wanted")
         return t.data_ptr()
 
-    def _rows(self, t, name, dtype, shape):
-        """(address, distance of the rows) of one whose rows may lie apart; 0: back to back."""
-        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index:
-            self._refuse(t, name, dtype, shape)
-        if t.is_contiguous():
-            return t.data_ptr(), 0
-        if t.stride(0) <= 0 or not t[0].is_contiguous():
-            raise ValueError(f"{name}: the elements of a row have to lie back to back")
-        return t.data_ptr(), t.stride(0)
-
-    def _refuse(self, t, name, dtype, shape):
-        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device} where {tuple(shape)} {dtype} on {self.device} is wanted")
+    def _rows(self, t, name, dtype, count, rows):
+        """(address, distance of the rows) of one whose rows, along its first dimension, may lie apart; 0: all elements lie back to back."""
+        if t.dtype is dtype and t.get_device() == self._index and t.numel() == count:
+            if t.is_contiguous():
+                return t.data_ptr(), 0
+            if t.shape[0] == rows and t.stride(0) > 0 and t[0].is_contiguous():
+                return t.data_ptr(), t.stride(0)
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device} where {rows} rows, back to back each, of {count} elements in all, {dtype} on {self.device} are wanted")
 
     def close(self) -> None:
         if getattr(self, "_handle", None):
@@ -895,23 +889,24 @@ class Norm(_Operator):
     def run_device(self, x, res=None, total=None, y=None, y8=None, scales=None) -> None:
         """x, res, total, y: CUDA [rows, dim] of the configuration's types, rows any distance apart; y8: float8_e4m3fn [rows, width8(dim)],
         scales: float8_e8m0fnu [rows, scale_columns(dim)].  Those that are None are not there.  Queued on the stream."""
-        shape, (x_type, res_type, y_type) = x.shape, self._types
-        if len(shape) != 2 or shape[1] != self._dim:
-            raise ValueError(f"x: {tuple(shape)} where [rows, {self._dim}] is wanted")
-        rows = shape[0]
+        x_type, res_type, y_type = self._types
+        count = x.numel()
+        rows, rest = divmod(count, self._dim)
+        if rest:
+            raise ValueError(f"x: {tuple(x.shape)} where rows of {self._dim} are wanted")
         a = TtsNormRows()
         a.rows = rows
-        a.x, a.x_stride = self._rows(x, "x", x_type, shape)
+        a.x, a.x_stride = self._rows(x, "x", x_type, count, rows)
         if res is not None:
-            a.res, a.res_stride = self._rows(res, "res", res_type, shape)
+            a.res, a.res_stride = self._rows(res, "res", res_type, count, rows)
         if total is not None:
-            a.total, a.total_stride = self._rows(total, "total", res_type, shape)
+            a.total, a.total_stride = self._rows(total, "total", res_type, count, rows)
         if y is not None:
-            a.y, a.y_stride = self._rows(y, "y", y_type, shape)
+            a.y, a.y_stride = self._rows(y, "y", y_type, count, rows)
         if y8 is not None:
-            a.y8 = self._at(y8, "y8", self._types8[0], (rows, self._widths[0]))
+            a.y8 = self._at(y8, "y8", self._types8[0], rows * self._widths[0])
         if scales is not None:
-            a.scales = self._at(scales, "scales", self._types8[1], (rows, self._widths[1]))
+            a.scales = self._at(scales, "scales", self._types8[1], rows * self._widths[1])
         rc = self._run(self._handle, a)
         if rc:
             _check(rc)
@@ -939,10 +934,12 @@ class Linear8(_Operator):
     def run_device(self, x8, scales, y) -> None:
         """x8: CUDA float8_e4m3fn [rows, width8(in_dim)], zeros past in_dim; scales: float8_e8m0fnu [rows, scale_columns(in_dim)]; y: [rows, out_dim],
         rows any distance apart.  Queued on the stream."""
-        rows, (k, n_scales, n) = x8.shape[0], self._widths
-        at = self._at(x8, "x8", self._types8[0], (rows, k))
-        sx = self._at(scales, "scales", self._types8[1], (rows, n_scales))
-        rc = self._run(self._handle, at, sx, rows, *self._rows(y, "y", self._y_type, (rows, n)))
+        k, n_scales, n = self._widths
+        rows = x8.numel() // k
+        at = self._at(x8, "x8", self._types8[0], rows * k)
+        sx = self._at(scales, "scales", self._types8[1], rows * n_scales)
+        to, apart = self._rows(y, "y", self._y_type, rows * n, rows)
+        rc = self._run(self._handle, at, sx, rows, to, apart)
         if rc:
             _check(rc)
 
@@ -973,7 +970,7 @@ class CrossAttention(_Operator):
         where = self._setup(cfg, stream, device)
         _check(lib().tts_cross_create(C.byref(cfg), *where))
         self._dtype = self._type(cfg.dtype)
-        self._heads = (cfg.n_heads, cfg.n_kv_heads, cfg.head_dim)
+        self._widths = (cfg.n_heads, cfg.n_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim)
 
     def batch(self, q_len, mem_row, mem_len) -> CrossBatch:
         """A batch's lengths, for any number of calls."""
@@ -982,20 +979,19 @@ class CrossAttention(_Operator):
     def run_device(self, batch: CrossBatch, q, k, v, out, keep=None, lse=None, scale: float = 0.0) -> None:
         """q, out: CUDA [queries, n_heads, head_dim]; k, v: [memory rows, n_kv_heads, head_dim], rows any multiple of 8 elements apart; keep: uint8
         [memory rows], 0 = hidden; lse: fp32 [queries, n_heads].  Queued on the stream; scale 0: 1 / sqrt(head_dim)."""
-        t, (heads, kv, d) = self._dtype, self._heads
-        rows = k.shape[0]
-        of_q, of_k = (batch.queries, heads, d), (rows, kv, d)
+        t, (heads, of_q, of_k) = self._dtype, self._widths
+        queries, rows = batch.queries, k.numel() // of_k
         if rows < batch.memory_rows:
             raise ValueError(f"k has {rows} rows, the batch's memories end at {batch.memory_rows}")
         a = TtsCrossTensors()
-        a.q, a.q_stride = self._rows(q, "q", t, of_q)
-        a.k, a.k_stride = self._rows(k, "k", t, of_k)
-        a.v, a.v_stride = self._rows(v, "v", t, of_k)
-        a.out, a.out_stride = self._rows(out, "out", t, of_q)
+        a.q, a.q_stride = self._rows(q, "q", t, queries * of_q, queries)
+        a.k, a.k_stride = self._rows(k, "k", t, rows * of_k, rows)
+        a.v, a.v_stride = self._rows(v, "v", t, rows * of_k, rows)
+        a.out, a.out_stride = self._rows(out, "out", t, queries * of_q, queries)
         if keep is not None:
-            a.keep = self._at(keep, "keep", self._torch.uint8, (rows,))
+            a.keep = self._at(keep, "keep", self._torch.uint8, rows)
         if lse is not None:
-            a.lse = self._at(lse, "lse", self._torch.float32, of_q[:2])
+            a.lse = self._at(lse, "lse", self._torch.float32, queries * heads)
         a.scale = scale
         rc = self._run(self._handle, batch.c, a)
         if rc:
