@@ -54,7 +54,7 @@ typedef struct {
 
 /* DEVICE pointers.  A row of q and out holds n_heads * head_dim elements, one of k and v n_kv_heads * head_dim; a stride is the distance between
  * rows in elements, a multiple of 8, at most 2^24 (0: the rows lie back to back).  q, k, v and out are
- * 16-byte aligned; k and v may be null where every mem_len is 0. */
+ * 16-byte aligned; k and v may be null where every mem_len is 0.  out and lse overlap nothing. */
 typedef struct {
     const void *q;  long long q_stride;
     const void *k;  long long k_stride;

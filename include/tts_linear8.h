@@ -54,7 +54,7 @@ int tts_linear8_create(const tts_linear8_config *cfg, const float *w, const floa
  *   scales  DEVICE [rows][TTS_SCALE_COLUMNS(in_dim)] bytes, 4-byte aligned
  *   y       DEVICE [rows] rows of out_dim elements, y_stride elements apart (0: out_dim), aligned to its element
  * Errors: TTS_E_INVAL for null pointers, rows outside 0 .. TTS_MAX_ROWS (tts_norm.h; 0 does nothing), a stride below out_dim or above 2^40,
- * or an array that is not aligned.
+ * or an array that is not aligned.  y overlaps neither of the others.
  */
 int tts_linear8_run(tts_linear8 *lin, const void *x8, const void *scales, int rows, void *y, long long y_stride);
 

@@ -165,6 +165,16 @@ template <typename T, int D, bool FULL, bool MASK> struct Running {
     }
 };
 
+// The request that tile `id` of a launch is of: the last whose tiles begin at or ahead of it.
+__device__ __forceinline__ int request_of(const CrossArgs& p, int id)
+{
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < CROSS_BATCH; i += 64) before += __popcll(__ballot(i + lane < p.n && p.req[min(i + lane, p.n - 1)].first <= id));
+    return __builtin_amdgcn_readfirstlane(before) - 1;
+}
+
 // D / 16 neighbouring columns of a row
 template <typename T, int NE> __device__ __forceinline__ void store_columns(T* at, const float* v)
 {
@@ -210,10 +220,9 @@ template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(
     constexpr int NE = G::NE, PITCH = D + 4, STRIDE = FEW_WAVES * G::N;
     __shared__ __align__(16) float s_o[FEW_WAVES][16][PITCH];
     __shared__ float s_ml[FEW_WAVES][2][16];
-    const CrossReq r = p.req[blockIdx.z];
-    const int kv = blockIdx.y, split = blockIdx.x % splits, tile = blockIdx.x / splits;
-    const int group = p.n_heads / p.n_kv_heads, rows = r.q_len * group;
-    if (16 * tile >= rows) return;
+    const int split = blockIdx.x % splits, id = blockIdx.x / splits, group = p.n_heads / p.n_kv_heads;
+    const CrossReq r = p.req[p.single ? id / p.n_kv_heads : request_of(p, id)];
+    const int rows = r.q_len * group, tiles = (rows + 15) / 16, kv = (id - r.first) / tiles, tile = (id - r.first) % tiles;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, g = lane >> 4;
     const int begin = split * share, end = min(r.mem_len, begin + share);
     if (split > 0 && begin >= r.mem_len) return;
@@ -269,7 +278,7 @@ template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(
         return;
     }
     // a part: rows of columns, then the rows' maxima and sums
-    float* part = p.parts + (((size_t)blockIdx.z * p.n_kv_heads + kv) * gridDim.x + blockIdx.x) * part_floats(D);
+    float* part = p.parts + (size_t)blockIdx.x * part_floats(D);
     float top = -__builtin_inff(), sum = 0, c[NE] = {};
 #pragma unroll
     for (int i = 0; i < FEW_WAVES; ++i) top = fmaxf(top, s_ml[i][0][in_tile]);
@@ -296,11 +305,12 @@ template <typename T, int D> __global__ __launch_bounds__(JOIN) void k_cross_joi
     constexpr int ACROSS = D / 4, GROUPS = JOIN / ACROSS;
     __shared__ float s_w[JOIN], s_top[JOIN / 64], s_sum[JOIN / 64];
     __shared__ float4 s_o[GROUPS][ACROSS];
-    const CrossReq r = p.req[blockIdx.z];
-    const int kv = blockIdx.y, tile = blockIdx.x / 16, in_tile = blockIdx.x % 16, group = p.n_heads / p.n_kv_heads, row = 16 * tile + in_tile;
-    if (row >= r.q_len * group) return;
+    const int id = blockIdx.x / 16, in_tile = blockIdx.x % 16, group = p.n_heads / p.n_kv_heads;
+    const CrossReq r = p.req[p.single ? id / p.n_kv_heads : request_of(p, id)];
+    const int rows = r.q_len * group, tiles = (rows + 15) / 16, kv = (id - r.first) / tiles, row = 16 * ((id - r.first) % tiles) + in_tile;
+    if (row >= rows) return;
     const int n_parts = max(1, (r.mem_len + share - 1) / share), wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-    const float* parts = p.parts + (((size_t)blockIdx.z * p.n_kv_heads + kv) * (gridDim.x / 16) + tile) * splits * part_floats(D);
+    const float* parts = p.parts + (size_t)id * splits * part_floats(D);
     const bool mine = (int)threadIdx.x < n_parts;
     const float* ml = parts + (size_t)(mine ? threadIdx.x : 0) * part_floats(D) + 16 * D + in_tile;
     const float m = mine ? ml[0] : -__builtin_inff(), l = mine ? ml[16] : 0.f;
@@ -383,8 +393,7 @@ template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW,
     // Which tile: an XCD has a run of them, so that its L2 holds the memory that they share
     const int xcd = blockIdx.x & 7, id = p.start[xcd] + (blockIdx.x >> 3);
     if (id >= p.start[xcd + 1]) return;
-    const uint64_t before0 = __ballot(lane < p.n && p.req[min(lane, p.n - 1)].first <= id), before1 = __ballot(64 + lane < p.n && p.req[min(64 + lane, p.n - 1)].first <= id);
-    const CrossReq r = p.req[__popcll(before0) + __popcll(before1) - 1];
+    const CrossReq r = p.req[request_of(p, id)];
     const int group = p.n_heads / p.n_kv_heads, rows = r.q_len * group, tiles = (rows + 32 * NW - 1) / (32 * NW);
     const int kv = (id - r.first) / tiles, row = ((id - r.first) % tiles * NW + wave) * 32 + c, row_there = min(row, rows - 1);
     const long long q_row = (long long)r.q_row + row_there / group;
@@ -574,21 +583,26 @@ template <int D, int NW, int R> hipError_t allow()
     return e == hipSuccess ? hipFuncSetAttribute(reinterpret_cast<const void*>(b), hipFuncAttributeMaxDynamicSharedMemorySize, ManyRows<D, NW, R>::LDS) : e;
 }
 
-template <int D, int NW, int R> void go_many(CrossArgs& a, hipStream_t s)
+template <int D, int NW, int R> hipError_t go_many(CrossArgs& a, hipStream_t s)
 {
     // shares of the XCDs: equal in keys that their tiles go over, and a tile's own cost, some 160 keys' (16 requests of 600 queries, 8 heads of 64, over 64 keys 7.5
     // us, over 250 12.8, of which 2 are the launch's)
     constexpr int OWN = 160;
     const int group = a.n_heads / a.n_kv_heads;
-    auto tiles_of = [&](const CrossReq& r) { return (int)(((long long)r.q_len * group + 32 * NW - 1) / (32 * NW)) * a.n_kv_heads; };
+    auto tiles_of = [&](const CrossReq& r) { return ((long long)r.q_len * group + 32 * NW - 1) / (32 * NW) * a.n_kv_heads; };
     double work = 0, done = 0;
+    long long all = 0;
     int tiles = 0, most = 0;
-    for (int i = 0; i < a.n; ++i) work += (double)tiles_of(a.req[i]) * (a.req[i].mem_len + OWN);
+    for (int i = 0; i < a.n; ++i) {
+        work += (double)tiles_of(a.req[i]) * (a.req[i].mem_len + OWN);
+        all += tiles_of(a.req[i]);
+    }
+    if (all > 0x7FFFFFFF / 8) return hipErrorInvalidValue;
     int x = 1;
     a.start[0] = 0;
     for (int i = 0; i < a.n; ++i) {
         a.req[i].first = tiles;
-        const int mine = tiles_of(a.req[i]), each = a.req[i].mem_len + OWN;
+        const int mine = (int)tiles_of(a.req[i]), each = a.req[i].mem_len + OWN;
         for (; x < 8 && done + (double)mine * each >= work * x / 8; ++x) a.start[x] = std::min(tiles + mine, std::max(a.start[x - 1], tiles + (int)((work * x / 8 - done) / each + 0.5)));
         tiles += mine;
         done += (double)mine * each;
@@ -598,33 +612,40 @@ template <int D, int NW, int R> void go_many(CrossArgs& a, hipStream_t s)
     const auto kernel = a.keep ? k_cross_many<D, NW, R, true> : k_cross_many<D, NW, R, false>;
     constexpr int LDS = ManyRows<D, NW, R>::LDS;
     hipLaunchKernelGGL(kernel, dim3(8 * most), dim3(64 * NW), LDS, s, a);
+    return hipGetLastError();
 }
 
-template <typename T, int D, bool FULL> void go_few(const CrossArgs& a, int n_cu, hipStream_t s)
+template <typename T, int D, bool FULL> hipError_t go_few(CrossArgs& a, int n_cu, hipStream_t s)
 {
-    int tiles = 0, longest = 0;
+    int longest = 0;
+    long long wgs = 0, rows_keys = 0;                    // row tiles, and the keys that they go over
     const int group = a.n_heads / a.n_kv_heads;
+    a.single = true;
     for (int i = 0; i < a.n; ++i) {
-        tiles = std::max(tiles, (a.req[i].q_len * group + 15) / 16);
+        const long long tiles = ((long long)a.req[i].q_len * group + 15) / 16;
+        a.single &= tiles == 1;
+        a.req[i].first = (int)wgs;
+        wgs += tiles * a.n_kv_heads;
+        rows_keys += tiles * a.n_kv_heads * a.req[i].mem_len;
         longest = std::max(longest, a.req[i].mem_len);
+        if (wgs > 0x7FFFFFFF) return hipErrorInvalidValue;
     }
     // A workgroup by itself takes its memory at 50 to 100 GB/s (some 0.6 us for a step of its four waves), the join's launch costs 3 us.  So a memory is split where
     // workgroups are few and it is long, into parts of equal length, of all requests alike, so that a round of them ends together.  us, whole / split, 8 heads of 64,
     // bf16, requests x keys: 1 x 500 5.7 / 7.1, 1 x 1000 8.3 / 7.1, 1 x 30000 - / 17.5, 8 x 1000 8.4 / 8.6, 8 x 4000 23.7 / 18.0, 16 x 4000 24.4 / 28.4, 16 x
     // 16000 153 / 119, 32 x 16000 209 / 231; 4 x 27000, 8 heads of 128 that four share each, 339 / 88 (5.05 TB/s).
-    const long long wgs = (long long)tiles * a.n_kv_heads * a.n, bytes = (long long)longest * D * sizeof(T);
+    const long long bytes = (long long)longest * D * sizeof(T);
     int splits = 1, share = std::max(longest, 1);
     if ((wgs <= n_cu / 4 && bytes >= 128 << 10) || (wgs <= n_cu / 2 && bytes >= 1 << 20)) {
-        long long keys = 0;
-        for (int i = 0; i < a.n; ++i) keys += a.req[i].mem_len;
-        const long long most = std::min<long long>(MAX_PARTS / wgs, MAX_SPLITS), even = keys * tiles * a.n_kv_heads / MAX_PARTS;
+        const long long most = std::min<long long>(MAX_PARTS / wgs, MAX_SPLITS), even = rows_keys / MAX_PARTS;
         share = (int)((std::max({even, (longest + most - 1) / most, 128LL}) + 31) / 32 * 32);
         splits = (longest + share - 1) / share;
         if (splits < 2) splits = 1, share = longest;
     }
     const auto kernel = a.keep ? k_cross_few<T, D, FULL, true> : k_cross_few<T, D, FULL, false>;
-    hipLaunchKernelGGL(kernel, dim3(tiles * splits, a.n_kv_heads, a.n), dim3(FEW_WAVES * 64), 0, s, a, splits, share);
-    if (splits > 1) hipLaunchKernelGGL((k_cross_join<T, D>), dim3(16 * tiles, a.n_kv_heads, a.n), dim3(JOIN), 0, s, a, splits, share);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs * splits), dim3(FEW_WAVES * 64), 0, s, a, splits, share);
+    if (splits > 1) hipLaunchKernelGGL((k_cross_join<T, D>), dim3(16 * (unsigned)wgs), dim3(JOIN), 0, s, a, splits, share);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -640,14 +661,13 @@ hipError_t allow_cross()
     return e;
 }
 
-hipError_t launch_cross_few(const CrossArgs& a, bool bf16, int n_cu, hipStream_t s)
+hipError_t launch_cross_few(CrossArgs& a, bool bf16, int n_cu, hipStream_t s)
 {
     const bool wide = a.head_dim > 64, full = a.head_dim % 64 == 0;
-    if (bf16 && wide) full ? go_few<bf16_t, 128, true>(a, n_cu, s) : go_few<bf16_t, 128, false>(a, n_cu, s);
-    else if (bf16) full ? go_few<bf16_t, 64, true>(a, n_cu, s) : go_few<bf16_t, 64, false>(a, n_cu, s);
-    else if (wide) full ? go_few<float, 128, true>(a, n_cu, s) : go_few<float, 128, false>(a, n_cu, s);
-    else full ? go_few<float, 64, true>(a, n_cu, s) : go_few<float, 64, false>(a, n_cu, s);
-    return hipGetLastError();
+    if (bf16 && wide) return full ? go_few<bf16_t, 128, true>(a, n_cu, s) : go_few<bf16_t, 128, false>(a, n_cu, s);
+    if (bf16) return full ? go_few<bf16_t, 64, true>(a, n_cu, s) : go_few<bf16_t, 64, false>(a, n_cu, s);
+    if (wide) return full ? go_few<float, 128, true>(a, n_cu, s) : go_few<float, 128, false>(a, n_cu, s);
+    return full ? go_few<float, 64, true>(a, n_cu, s) : go_few<float, 64, false>(a, n_cu, s);
 }
 
 hipError_t launch_cross_many(CrossArgs& a, int n_cu, hipStream_t s)
@@ -662,9 +682,8 @@ hipError_t launch_cross_many(CrossArgs& a, int n_cu, hipStream_t s)
         longest = std::max(longest, a.req[i].mem_len);
     }
     const bool eight = longest >= 1024 && large >= n_cu - n_cu / 4;
-    if (a.head_dim > 64) eight ? go_many<128, 8, 3>(a, s) : go_many<128, 4, 2>(a, s);
-    else eight ? go_many<64, 8, 3>(a, s) : go_many<64, 4, 3>(a, s);
-    return hipGetLastError();
+    if (a.head_dim > 64) return eight ? go_many<128, 8, 3>(a, s) : go_many<128, 4, 2>(a, s);
+    return eight ? go_many<64, 8, 3>(a, s) : go_many<64, 4, 3>(a, s);
 }
 
 }  // namespace tts

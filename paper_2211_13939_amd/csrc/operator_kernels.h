@@ -41,7 +41,7 @@ constexpr int CROSS_BATCH = 128;         // requests of a launch
 struct CrossReq {
     long long mem_row;
     int mem_len, q_row, q_len;
-    int first;                           // of its row tiles, of all key heads, in the launch of many rows
+    int first;                           // of its row tiles, of all key heads, in the launch
 };
 struct CrossArgs {
     const void *q, *k, *v;
@@ -53,13 +53,14 @@ struct CrossArgs {
     float scale;                         // times log2(e)
     int n_heads, n_kv_heads, head_dim;
     int n;
-    int start[9];                        // of the row tiles that each XCD takes
+    bool single;                         // few rows: every request has one row tile
+    int start[9];                        // many rows: first of the row tiles that each XCD takes
     CrossReq req[CROSS_BATCH];
 };
 size_t cross_parts_bytes();
 hipError_t allow_cross();                // once on each device, before the first launch there
-// `few`: 16 rows a workgroup, both types; `many`: 128 or 256, two bytes alone (fills in what the launch's tiles are)
-hipError_t launch_cross_few(const CrossArgs& a, bool bf16, int n_cu, hipStream_t s);
+// `few`: 16 rows a workgroup, both types; `many`: 128 or 256, two bytes alone.  They fill in what the launch's tiles are.
+hipError_t launch_cross_few(CrossArgs& a, bool bf16, int n_cu, hipStream_t s);
 hipError_t launch_cross_many(CrossArgs& a, int n_cu, hipStream_t s);
 // A request is the latter's from two of the former's row tiles up, if the call has two and a half of those for every compute unit.  us, few / many: 16
 // requests, 8 heads of 64, 135 keys: 64 queries each (512 tiles) 5.4 / 6.5, 96 (768) 6.9 / 7.0, 192 (1536) 11.7 / 7.4; one of 1000 over 1000 keys (504) 20.7 /

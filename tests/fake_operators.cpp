@@ -50,7 +50,7 @@ static hipError_t launched(const CrossArgs& a)
     for (int i = 0; i < a.n; ++i) requests_seen += 1;
     return call("launch");
 }
-hipError_t launch_cross_few(const CrossArgs& a, bool, int, hipStream_t) { return launched(a); }
+hipError_t launch_cross_few(CrossArgs& a, bool, int, hipStream_t) { return launched(a); }
 hipError_t launch_cross_many(CrossArgs& a, int, hipStream_t)
 {
     ++many_launches;
