@@ -76,7 +76,8 @@ int tts_cross_create(const tts_cross_config *cfg, void *dev_arena, size_t arena_
 
 /*
  * Attend, asynchronously on the stream (the batch's arrays are consumed before the call returns).
- * Errors: TTS_E_INVAL for null pointers, a number of requests, a length or a row outside its range, more than 2^31 - 1 queries in all,
+ * Errors: TTS_E_INVAL for null pointers, a number of requests, a length or a row outside its range, more than 2^31 - 1 queries or 2^23 tiles in all
+ * (a tile: 16 pairs of a query and a head, of one request and one head of k),
  * a stride that is too small, too large or no multiple of 8, an array that is not aligned, or a scale that is negative or not finite.
  */
 int tts_cross_run(tts_cross *att, const tts_cross_batch *batch, const tts_cross_tensors *tensors);

@@ -119,6 +119,7 @@ extern "C" int tts_cross_run(tts_cross* p, const tts_cross_batch* b, const tts_c
     const bool bf16 = p->cfg.dtype == TTS_DTYPE_BF16;
     long long few_tiles = 0;
     for (int i = 0; i < b->n; ++i) few_tiles += ((long long)b->q_len[i] * group + 15) / 16 * p->cfg.n_kv_heads;
+    if (few_tiles > CROSS_MAX_TILES) return fail(TTS_E_INVAL, "%lld tiles of 16 rows in one call", few_tiles);
     const bool any_many = bf16 && cross_many(few_tiles, p->n_cu);
     for (int many = 0; many < 1 + any_many; ++many) {
         int q_row = 0;

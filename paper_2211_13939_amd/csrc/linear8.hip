@@ -130,8 +130,8 @@ template <typename YT> __global__ __launch_bounds__(FEW_WAVES * 64) void k_linea
 
 // Many rows: tiles of 32 * TN * WN channels and 32 * TM * WM rows, in steps of 64 * SUB columns.  A step of both operands lies in LDS while the next
 // STEPS - 1 are on their way there, 16 bytes a lane straight from memory; one barrier a step.  Weights lie in operand order.  Of x four
-// lanes bring the 64 bytes of a row (lanes of rows apart, as the operand has them, take a cycle of the load path each: 256 x 256 tiles of
-// 16384 x 4096 x 4096 in 277 us), each the quarter that its place is for: rows' quarters change places every four rows, so that the
+// lanes bring the 64 bytes of a row (lanes of rows apart, as the operand has them, take a cycle of the load path each: 128 x 128 tiles of
+// 16384 x 4096 x 4096 353 in place of 305 us), each the quarter that its place is for: rows' quarters change places every four rows, so that the
 // operand's reads of 16 bytes find all banks.
 //
 // These loads are written out: of the builtin the compiler does not know which of two buffers it fills, and waits for it in front of every read of the

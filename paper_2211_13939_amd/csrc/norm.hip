@@ -119,7 +119,7 @@ template <typename XT, typename RT, int LPR, int NC> __global__ __launch_bounds_
     constexpr int ROWS = 256 / LPR;
     __shared__ float part[LPR > 64 ? LPR / 64 : 1];
     const int lane = threadIdx.x % LPR;
-    const int row = blockIdx.x * ROWS + (LPR == 256 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / LPR));
+    const int row = (blockIdx.y * gridDim.x + blockIdx.x) * ROWS + (LPR == 256 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / LPR));
     if (row >= p.rows) return;
     const XT* x = static_cast<const XT*>(p.x) + row * p.x_stride;
     const RT* res = p.res ? static_cast<const RT*>(p.res) + row * p.res_stride : nullptr;
@@ -223,7 +223,8 @@ template <typename XT, typename RT, int LPR, int NC> __global__ __launch_bounds_
 template <int LPR, int NC> void go(const NormArgs& a, bool x_bf16, bool res_bf16, hipStream_t s)
 {
     constexpr int ROWS = 256 / LPR;
-    const dim3 grid((a.rows + ROWS - 1) / ROWS), block(256);
+    const int wgs = (a.rows + ROWS - 1) / ROWS, high = (wgs >> 23) + 1;       // (a grid has fewer than 2^32 threads a side)
+    const dim3 grid((wgs + high - 1) / high, high), block(256);
     if (x_bf16 && res_bf16) hipLaunchKernelGGL((k_norm<bf16_t, bf16_t, LPR, NC>), grid, block, 0, s, a);
     else if (x_bf16) hipLaunchKernelGGL((k_norm<bf16_t, float, LPR, NC>), grid, block, 0, s, a);
     else if (res_bf16) hipLaunchKernelGGL((k_norm<float, bf16_t, LPR, NC>), grid, block, 0, s, a);

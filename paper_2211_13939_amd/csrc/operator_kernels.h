@@ -66,6 +66,7 @@ hipError_t launch_cross_many(CrossArgs& a, int n_cu, hipStream_t s);
 // requests, 8 heads of 64, 135 keys: 64 queries each (512 tiles) 5.4 / 6.5, 96 (768) 6.9 / 7.0, 192 (1536) 11.7 / 7.4; one of 1000 over 1000 keys (504) 20.7 /
 // 19.4, with 16 heads of 128 that share 4 (1000) 41 / 24; 32 requests of 40 queries over 300, 8 heads that share one (640) 9.2 / 8.8.
 constexpr int CROSS_MANY_ROWS = 33;
+constexpr int CROSS_MAX_TILES = 1 << 23;     // a grid has fewer than 2^32 threads, and XCDs' shares of the tiles may be of different heights
 inline bool cross_many(long long few_tiles, int n_cu) { return 2 * few_tiles >= 5LL * n_cu; }
 
 }  // namespace tts

@@ -156,3 +156,25 @@ def test_no_rows_and_a_graph_of_another_streams_tensors():
         torch.cuda.synchronize()
         assert torch.equal(got, y) and torch.equal(got_t, total), k
     op.close()
+
+
+def test_as_many_rows_as_a_call_may_have():
+    """2^24 rows of a workgroup each: more than one side of a grid takes."""
+    import torch
+    rows, dim = 1 << 24, 2049
+    if torch.cuda.mem_get_info()[0] < 130 << 30:
+        pytest.skip("110 GB")
+    x = torch.zeros(rows, dim, dtype=torch.bfloat16, device="cuda:0")
+    at = [0, 1, (1 << 23) - 1, 1 << 23, (1 << 23) + 1, rows - 1]
+    some = _make(torch, np.random.default_rng(3), len(at), dim, True)
+    x[at] = some
+    op = binding.Norm(binding.make_norm_config(dim, True, kind=binding.NORM_NONE), stream=torch.cuda.current_stream())
+    y8 = torch.empty(rows, binding.width8(dim), dtype=torch.float8_e4m3fn, device="cuda:0")
+    sc = torch.empty(rows, binding.scale_columns(dim), dtype=torch.float8_e8m0fnu, device="cuda:0")
+    y8.view(torch.uint8).fill_(1)
+    op.run_device(x, y8=y8, scales=sc)
+    torch.cuda.synchronize()
+    want, want_s = ref.round8(_np(some))
+    np.testing.assert_array_equal(y8.view(torch.uint8)[at].cpu().numpy(), want)
+    np.testing.assert_array_equal(sc.view(torch.uint8)[at].cpu().numpy(), want_s)
+    assert int(y8.view(torch.uint8).view(-1).view(torch.int64).ne(0).view(rows, -1).any(1).sum()) == len(at)

@@ -231,12 +231,13 @@ def test_cross_refuses(lib):
     assert lib.fake_launches() == 2 and lib.fake_many() == 1 and lib.fake_requests_seen() == 140 and lib.fake_rows() == 70 * 501
     lib.fake_reset()
     assert run(q_len=[500] * 300, row=[0] * 300, mem=[1] * 300) == 0 and lib.fake_launches() == lib.fake_many() == 3 and lib.fake_requests_seen() == 300
+    assert run(q_len=[1 << 24], row=[0], mem=[1]) == 0                # 2^23 tiles of 16 rows
     assert run(scale=0.5) == 0 and run(k_stride=1 << 24, q_stride=328, row=(1 << 40, 0, 0)) == 0
     for change in (dict(n=0), dict(n=-1), dict(null="q_len"), dict(null="mem_row"), dict(null="mem_len"), dict(q_len=(-1, 0, 0)), dict(q_len=((1 << 24) + 1, 0, 0)), dict(mem=(-1, 0, 0)),
                    dict(mem=((1 << 24) + 1, 0, 0)), dict(row=(-1, 0, 0)), dict(row=((1 << 40) + 1, 0, 0)), dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(q_stride=319), dict(q_stride=321),
                    dict(k_stride=72), dict(v_stride=-80), dict(out_stride=(1 << 24) + 8), dict(q=(1 << 20) + 8), dict(k=(2 << 20) + 2), dict(v=(3 << 20) + 4), dict(out=(4 << 20) + 8),
                    dict(lse=(6 << 20) + 2), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(q_len=[1 << 24] * 129, row=[0] * 129, mem=[1] * 129),
-                   dict(q_len=[1] * 1025, row=[0] * 1025, mem=[1] * 1025)):
+                   dict(q_len=[1 << 24, 1], row=[0] * 2, mem=[1] * 2), dict(q_len=[1] * 1025, row=[0] * 1025, mem=[1] * 1025)):
         assert run(**change) == INVAL, change
         assert lib.tts_last_error()
     assert lib.tts_cross_run(None, None, None) == INVAL and lib.tts_cross_run(m.h, None, None) == INVAL
