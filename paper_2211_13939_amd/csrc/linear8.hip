@@ -150,25 +150,22 @@ template <int N> __device__ __forceinline__ void arrived()
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
 
-// 16 neighbouring channels of a row
-struct __attribute__((packed, aligned(2))) Eight16 { uint32_t w[4]; };
-template <typename YT> __device__ __forceinline__ void store_sixteen(const Linear8Args& p, int row, int n0, const floatx16& v)
+// 16 bytes of a row
+struct __attribute__((packed, aligned(2))) Piece { uint32_t w[4]; };
+template <typename YT> __device__ __forceinline__ void store_piece(const Linear8Args& p, int row, int n0, uint4 v)
 {
+    constexpr int N = 16 / sizeof(YT);
     if (row >= p.rows || n0 >= p.out_dim) return;
     YT* y = static_cast<YT*>(p.y) + row * p.y_stride + n0;
-    if (n0 + 16 <= p.out_dim) {
-        if constexpr (sizeof(YT) == 2) {
+    if (n0 + N <= p.out_dim) *reinterpret_cast<Piece*>(y) = Piece{{v.x, v.y, v.z, v.w}};
+    else {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int i = 0; i < 16; i += 8)
-                *reinterpret_cast<Eight16*>(y + i) = Eight16{{pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]), pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7])}};
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) *reinterpret_cast<Four32*>(y + i) = Four32{{v[i], v[i + 1], v[i + 2], v[i + 3]}};
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 15; ++i)
-            if (n0 + i < p.out_dim) y[i] = from_float<YT>(v[i]);
+        for (int i = 0; i < N - 1; ++i)
+            if (n0 + i < p.out_dim) {
+                if constexpr (sizeof(YT) == 2) reinterpret_cast<uint16_t*>(y)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+                else reinterpret_cast<uint32_t*>(y)[i] = w[i];
+            }
     }
 }
 
@@ -179,15 +176,17 @@ template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS> struc
     static constexpr int W_LOADS = SUB * NT * 2 / WAVES, X_LOADS = SUB * MT * 2 / WAVES, LOADS = W_LOADS + X_LOADS;      // of a wave a step
     static constexpr int S_LOADS = ((NT + MT) / 2 + WAVES - 1) / WAVES;                      // ... every four blocks
     static_assert(W_LOADS * WAVES == SUB * NT * 2 && X_LOADS * WAVES == SUB * MT * 2 && SUB <= 2 && NT % 2 == 0 && MT % 2 == 0, "shares of the waves");
+    static constexpr int PITCH = NT * 32 * sizeof(YT) + 16;                                 // of rows on their way out
+    static_assert(32 * WM * PITCH <= STEPS * STEP && 64 * WAVES % (NT * 2 * sizeof(YT)) == 0, "the results' way out");
     const Linear8Args& p;
     int wave, lane, wn, wm, unit0, row0;
     uint32_t lds_at;
     const uint8_t *w_at[W_LOADS], *x_at, *s_base[S_LOADS];      // this wave's share of a step, and of the scales
     uint32_t x_off[X_LOADS], s_off[S_LOADS], s_step[S_LOADS];
-    const uint8_t* lds;
+    uint8_t* lds;
     floatx16 acc[TN * TM] = {};
 
-    __device__ __forceinline__ Many(const Linear8Args& a, const uint8_t* l, int n_tile, int m_tile) : p(a), lds(l)
+    __device__ __forceinline__ Many(const Linear8Args& a, uint8_t* l, int n_tile, int m_tile) : p(a), lds(l)
     {
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         lane = threadIdx.x & 63;
@@ -277,6 +276,8 @@ template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS> struc
             if (n + 1 < TN) w = next;
         }
     }
+    // first of a lane's 16 channels of a unit
+    __device__ __forceinline__ int channel(int unit) const { return unit / 2 * 64 + 32 * (lane >> 5) + 16 * (unit & 1); }
     __device__ __forceinline__ void run()
     {
         constexpr int PER_WORD = 8 / SUB;
@@ -303,13 +304,35 @@ template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS> struc
             slot = slot + 1 == STEPS ? 0 : slot + 1;
         }
         settle(acc);
+        // Rows leave by way of LDS, 32 * WM of them at a time, 16 bytes a lane along a row: lanes as the products have them would write to 64 lines an
+        // instruction, a cycle each.
+        floatx16 bias[TN] = {};
 #pragma unroll
         for (int n = 0; n < TN; ++n) {
-            const int u = unit0 + wn * TN + n, n0 = u / 2 * 64 + 32 * (lane >> 5) + 16 * (u & 1);
-            floatx16 bias = {};
-            if (n0 < p.out_dim) bias = *reinterpret_cast<const floatx16*>(p.bias + n0);
+            const int n0 = channel(wn * TN + n);
+            if (unit0 * 32 + n0 < p.out_dim) bias[n] = *reinterpret_cast<const floatx16*>(p.bias + unit0 * 32 + n0);
+        }
 #pragma unroll
-            for (int m = 0; m < TM; ++m) store_sixteen<YT>(p, row0 + (wm * TM + m) * 32 + (lane & 31), n0, acc[n * TM + m] + bias);
+        for (int m = 0; m < TM; ++m) {
+            __syncthreads();                              // (steps, and the rows before these, are read)
+#pragma unroll
+            for (int n = 0; n < TN; ++n) {
+                uint8_t* to = lds + (wm * 32 + (lane & 31)) * PITCH + channel(wn * TN + n) * sizeof(YT);
+                const floatx16 v = acc[n * TM + m] + bias[n];
+#pragma unroll
+                for (int i = 0; i < 16; i += 16 / sizeof(YT)) {
+                    if constexpr (sizeof(YT) == 2)
+                        *reinterpret_cast<uint4*>(to + 2 * i) = make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]), pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
+                    else *reinterpret_cast<float4*>(to + 4 * i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                }
+            }
+            __syncthreads();
+            constexpr int ACROSS = NT * 32 * sizeof(YT) / 16, ROWS = 64 * WAVES / ACROSS;
+#pragma unroll
+            for (int i = 0; i < 32 * WM / ROWS; ++i) {
+                const int r = i * ROWS + threadIdx.x / ACROSS, at = threadIdx.x % ACROSS;
+                store_piece<YT>(p, row0 + (r / 32 * TM + m) * 32 + r % 32, unit0 * 32 + at * (16 / (int)sizeof(YT)), *reinterpret_cast<const uint4*>(lds + r * PITCH + 16 * at));
+            }
         }
     }
 };
