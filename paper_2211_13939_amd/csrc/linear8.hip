@@ -487,6 +487,9 @@ template <typename YT> hipError_t go(const Linear8Args& a, int n_cu, hipStream_t
     auto tiles = [&](int n, int m) { return (long long)((units + n - 1) / n) * ((a.rows + 32 * m - 1) / (32 * m)); };
     const int enough = 2 * n_cu;
     if (tiles(1, 1) <= enough) return go_split<YT, 1, 2>(a, s);
+    // (few columns: a workgroup is its first loads and its results, of which more, smaller ones have more at once.  64 x 128 rows against the largest: 16384 x 512 x 2048 32.0 /
+    // 35.5 us, 4096 x 256 x 1024 5.2 / 6.5; 16384 x 640 x 2048 38.6 / 34.9.)
+    if (a.blocks <= 4 && tiles(2, 4) >= enough) return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
     if (tiles(8, 4) >= enough) return go_many<YT, 4, 2, 2, 2, 1, 3>(a, s);
     if (tiles(4, 4) >= enough) return go_many<YT, 2, 2, 2, 2, 2, 2>(a, s);
     if (tiles(2, 4) >= enough) return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);

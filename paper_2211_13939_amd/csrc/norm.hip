@@ -15,6 +15,15 @@ namespace {
 // Eight elements from an address that is aligned to its elements alone (the hardware takes wide accesses at any address): rows
 // of odd widths cost no loads of single elements but in their last chunk.
 struct __attribute__((packed, aligned(2))) Raw16 { uint32_t w[4]; };
+typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(2)));
+// LATER: what this writes is read some kernels later (total, by the next norm): past the caches, which leaves them to what the next product reads.  bf16, a norm and
+// the product of its rows by square weights in turn, us before / after: 2000 x 512 8.6 / 8.6, 8192 x 1024 26.5 / 27.6, 8192 x 2048 60.6 / 58.3, 16384 x 2048 109.8 /
+// 105.9; a norm by itself, 6831 x 448 7.0 / 5.8.  (y and y8 so as well: 28.7, 60.9 and 112.8 us of the same; they are read next.)
+template <bool LATER> __device__ __forceinline__ void put(void* p, const Raw16& a)
+{
+    if constexpr (LATER) __builtin_nontemporal_store(Words4{a.w[0], a.w[1], a.w[2], a.w[3]}, static_cast<Words4*>(p));
+    else *static_cast<Raw16*>(p) = a;
+}
 
 template <typename T> struct Eight;
 template <> struct Eight<float> {
@@ -52,8 +61,7 @@ template <> struct Eight<bf16_t> {
     __device__ __forceinline__ float get(int i) const { return i & 1 ? bf16_hi(a.w[i >> 1]) : bf16_lo(a.w[i >> 1]); }
 };
 
-template <typename T> __device__ __forceinline__ void store_eight(T* p, const float* v, int n);
-template <> __device__ __forceinline__ void store_eight<float>(float* p, const float* v, int n)
+template <bool LATER> __device__ __forceinline__ void store_eight(float* p, const float* v, int n)
 {
     if (n >= 8) {
         Raw16 a, b;
@@ -62,21 +70,21 @@ template <> __device__ __forceinline__ void store_eight<float>(float* p, const f
             a.w[i] = __float_as_uint(v[i]);
             b.w[i] = __float_as_uint(v[4 + i]);
         }
-        *reinterpret_cast<Raw16*>(p) = a;
-        *reinterpret_cast<Raw16*>(p + 4) = b;
+        put<LATER>(p, a);
+        put<LATER>(p + 4, b);
     } else {
 #pragma unroll
         for (int i = 0; i < 7; ++i)
             if (i < n) p[i] = v[i];
     }
 }
-template <> __device__ __forceinline__ void store_eight<bf16_t>(bf16_t* p, const float* v, int n)
+template <bool LATER> __device__ __forceinline__ void store_eight(bf16_t* p, const float* v, int n)
 {
     if (n >= 8) {
         Raw16 a;
 #pragma unroll
         for (int i = 0; i < 4; ++i) a.w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<Raw16*>(p) = a;
+        put<LATER>(p, a);
     } else {
 #pragma unroll
         for (int i = 0; i < 7; ++i)
@@ -163,7 +171,7 @@ template <typename XT, typename RT, int LPR, int NC> __global__ __launch_bounds_
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int at = (c * LPR + lane) * 8;
-            if (at < p.dim) store_eight<RT>(total + at, t[c], p.dim - at);
+            if (at < p.dim) store_eight<true>(total + at, t[c], p.dim - at);
         }
     }
     if (!p.y && !p.y8) return;
@@ -191,8 +199,8 @@ template <typename XT, typename RT, int LPR, int NC> __global__ __launch_bounds_
         for (int c = 0; c < NC; ++c) {
             const int at = (c * LPR + lane) * 8;
             if (at >= p.dim) continue;
-            if (p.y_bf16) store_eight<bf16_t>(static_cast<bf16_t*>(p.y) + row * p.y_stride + at, t[c], p.dim - at);
-            else store_eight<float>(static_cast<float*>(p.y) + row * p.y_stride + at, t[c], p.dim - at);
+            if (p.y_bf16) store_eight<false>(static_cast<bf16_t*>(p.y) + row * p.y_stride + at, t[c], p.dim - at);
+            else store_eight<false>(static_cast<float*>(p.y) + row * p.y_stride + at, t[c], p.dim - at);
         }
     }
     if (p.y8) {
