@@ -480,20 +480,31 @@ template <typename YT> hipError_t go(const Linear8Args& a, int n_cu, hipStream_t
         hipLaunchKernelGGL((k_linear8_few<YT>), dim3(2 * units), dim3(FEW_WAVES * 64), 0, s, a);
         return hipGetLastError();
     }
-    // Otherwise the largest tile that leaves two workgroups for every compute unit: a larger one asks for fewer bytes, a smaller one has its latencies
-    // spread over more.  us, two-byte results, 32 x 32 split / 64 x 64 / 64 channels x 128 rows / 128 x 128 / 256 x 128: 512 x 1024 x 1024 4.5 / 4.8 / 5.6 /
-    // 7.8 / 12.5; 1024 x 2048 x 2048 17.6 / 8.6 / 9.7 / 12.6 / 20.5; 4096 x 1024 x 1024 - / 11.6 / 9.5 / 10.1 / 14.1; 4096 x 2048 x 2048 - / 31.4 / 28.0 / 22.7 /
-    // 24.9; 16384 x 1024 x 1024 - / 34.9 / 30.1 / 28.6 / 26.3; 16384 x 4096 x 4096 - / 423 / 352 / 275 / 244.
+    // Otherwise tiles: a larger one asks for fewer bytes, a smaller one has its latencies spread over more workgroups.  us, two-byte results, 32 x 32 split / 64 x 64 / 64
+    // channels x 128 rows / 128 x 128 / 256 x 128: 200 x 2048 x 2048 5.7 / 6.6 / 8.3 / 12.3 / 20.6; 512 x 2048 x 2048 10.0 / 6.9 / 8.4 / 12.5 / 20.7; 1024 x 2048 x 2048 17.0 / 8.4 /
+    // 9.2 / 12.5 / 20.9; 1542 x 2048 x 2048 - / 15.6 / 11.5 / 13.6 / 21.2; 3500 x 2048 x 2048 - / 25.7 / 25.6 / 19.5 / 22.9; 8000 x 1024 x 1024 - / 16.3 / 15.1 / 13.1 / 16.0; 16384 x
+    // 1024 x 1024 - / 33.0 / 27.1 / 27.4 / 24.9; 16384 x 4096 x 4096 - / 427 / 358 / 278 / 251.
     auto tiles = [&](int n, int m) { return (long long)((units + n - 1) / n) * ((a.rows + 32 * m - 1) / (32 * m)); };
-    const int enough = 2 * n_cu;
-    if (tiles(1, 1) <= enough) return go_split<YT, 1, 2>(a, s);
+    const int two = 2 * n_cu;
+    if (tiles(1, 1) <= two) return go_split<YT, 1, 2>(a, s);
     // (few columns: a workgroup is its first loads and its results, of which more, smaller ones have more at once.  64 x 128 rows against the largest: 16384 x 512 x 2048 32.0 /
     // 35.5 us, 4096 x 256 x 1024 5.2 / 6.5; 16384 x 640 x 2048 38.6 / 34.9.)
-    if (a.blocks <= 4 && tiles(2, 4) >= enough) return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
-    if (tiles(8, 4) >= enough) return go_many<YT, 4, 2, 2, 2, 1, 3>(a, s);
-    if (tiles(4, 4) >= enough) return go_many<YT, 2, 2, 2, 2, 2, 2>(a, s);
-    if (tiles(2, 4) >= enough) return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
-    return go_many<YT, 1, 1, 2, 2, 2, 3>(a, s);
+    if (a.blocks <= 4 && tiles(2, 4) >= two) return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
+    if constexpr (sizeof(YT) == 2) {
+        // The smallest that goes round once with two workgroups a compute unit: what comes in a second round costs a whole one.
+        if (tiles(2, 2) <= two) return go_many<YT, 1, 1, 2, 2, 2, 3>(a, s);
+        if (tiles(2, 4) <= two) return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
+        if (tiles(4, 4) <= two) return go_many<YT, 2, 2, 2, 2, 2, 2>(a, s);
+        return go_many<YT, 4, 2, 2, 2, 1, 3>(a, s);
+    } else {
+        // Operands' way to bf16 keeps the vector pipes busy, and several workgroups a compute unit even out.  The largest that leaves two of them: us, 64 x 64 / 64 x 128 / 128 x
+        // 128 / 256 x 128: 1280 x 2048 x 2048 17.5 / 18.6 / 19.9 / 33.7, 3000 x 2048 x 2048 32.9 / 30.5 / 31.9 / 35.4, 3000 x 4096 x 4096 115 / 102 / 94 / 102, 16384 x 4096 x
+        // 4096 657 / 550 / - / 460.  (64 x 64 with two steps in LDS, four workgroups a compute unit: 1542 x 2048 x 2048 23.8 -> 21.7.)
+        if (tiles(8, 4) >= two) return go_many<YT, 4, 2, 2, 2, 1, 3>(a, s);
+        if (tiles(4, 4) >= two) return go_many<YT, 2, 2, 2, 2, 2, 2>(a, s);
+        if (tiles(2, 4) >= two) return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
+        return go_many<YT, 1, 1, 2, 2, 2, 2>(a, s);
+    }
 }
 
 }  // namespace
@@ -505,7 +516,7 @@ template <typename YT> static hipError_t allow_all()
     if (e == hipSuccess) e = allow<YT, 4, 2, 2, 2, 1, 3>();
     if (e == hipSuccess) e = allow<YT, 2, 2, 2, 2, 2, 2>();
     if (e == hipSuccess) e = allow<YT, 1, 2, 2, 2, 2, 2>();
-    if (e == hipSuccess) e = allow<YT, 1, 1, 2, 2, 2, 3>();
+    if (e == hipSuccess) e = allow<YT, 1, 1, 2, 2, 2, sizeof(YT) == 2 ? 3 : 2>();
     return e;
 }
 hipError_t allow_linear8()
