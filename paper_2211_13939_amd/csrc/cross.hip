@@ -9,6 +9,7 @@
 #include "mfma.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace tts {
@@ -16,7 +17,7 @@ namespace tts {
 namespace {
 
 constexpr int FEW_WAVES = 4;
-constexpr int MAX_PARTS = 1024, MAX_SPLITS = 256;    // parts of one launch, of one row tile
+constexpr int MAX_PARTS = 2048, MAX_SPLITS = 256;    // parts of one launch, of one row tile
 constexpr int part_floats(int d) { return 16 * (d + 2); }
 
 // of the four lanes that share l % 16
@@ -94,6 +95,8 @@ template <typename T, int D, bool FULL, bool MASK> struct Keys {
 #pragma unroll
                 for (size_t b = 0; b < G::NE * sizeof(T); b += 16) *reinterpret_cast<uint4*>(v[i] + b / 4) = *reinterpret_cast<const uint4*>(vp + from + b);
         }
+        // (left alone, the compiler puts them in front of their use: 26 requests of 2185 .. 2925 keys, 8 fp32 heads of 128, 171 in place of 101 us)
+        if constexpr (MASK) __builtin_amdgcn_sched_barrier(0);
     }
     __device__ __forceinline__ void scores(const uint4 (&q)[G::NF], float* s) const
     {
@@ -165,15 +168,18 @@ template <typename T, int D, bool FULL, bool MASK> struct Running {
     }
 };
 
-// The request that tile `id` of a launch is of: the last whose tiles begin at or ahead of it.
-__device__ __forceinline__ int request_of(const CrossArgs& p, int id)
+// The request that tile (row) `id` of a launch is of: the last whose tiles (rows) begin at or ahead of it.
+template <int CrossReq::* FIRST = &CrossReq::first> __device__ __forceinline__ int request_of(const CrossArgs& p, int id)
 {
     const int lane = threadIdx.x & 63;
     int before = 0;
 #pragma unroll
-    for (int i = 0; i < CROSS_BATCH; i += 64) before += __popcll(__ballot(i + lane < p.n && p.req[min(i + lane, p.n - 1)].first <= id));
+    for (int i = 0; i < CROSS_BATCH; i += 64) before += __popcll(__ballot(i + lane < p.n && p.req[min(i + lane, p.n - 1)].*FIRST <= id));
     return __builtin_amdgcn_readfirstlane(before) - 1;
 }
+
+// (one without keys, too, where there are none)
+__host__ __device__ __forceinline__ int parts_of(const CrossReq& r, int share) { return r.mem_len <= share ? 1 : (r.mem_len - 1) / share + 1; }
 
 // D / 16 neighbouring columns of a row
 template <typename T, int NE> __device__ __forceinline__ void store_columns(T* at, const float* v)
@@ -214,18 +220,24 @@ __device__ __forceinline__ void finish_row(const CrossArgs& p, const CrossReq& r
 }
 
 // A tile of 16 rows over a part of its request's memory; the waves take steps of keys in turn, the next one's on its way, and meet in LDS.
-template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(FEW_WAVES * 64) void k_cross_few(CrossArgs p, int splits, int share)
+template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(FEW_WAVES * 64) void k_cross_few(CrossArgs p)
 {
     using G = Geometry<T, D>;
     constexpr int NE = G::NE, PITCH = D + 4, STRIDE = FEW_WAVES * G::N;
     __shared__ __align__(16) float s_o[FEW_WAVES][16][PITCH];
     __shared__ float s_ml[FEW_WAVES][2][16];
-    const int split = blockIdx.x % splits, id = blockIdx.x / splits, group = p.n_heads / p.n_kv_heads;
+    const int id = p.runs ? (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3) : blockIdx.x, group = p.n_heads / p.n_kv_heads;
+    if (id >= p.items) return;
     const CrossReq r = p.req[p.single ? id / p.n_kv_heads : request_of(p, id)];
-    const int rows = r.q_len * group, tiles = (rows + 15) / 16, kv = (id - r.first) / tiles, tile = (id - r.first) % tiles;
+    int at_tile = id - r.first, split = 0;
+    if (p.share) {
+        const int parts = parts_of(r, p.share);
+        split = at_tile % parts;
+        at_tile /= parts;
+    }
+    const int rows = r.q_len * group, tiles = (rows + 15) / 16, kv = at_tile / tiles, tile = at_tile % tiles;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, g = lane >> 4;
-    const int begin = split * share, end = min(r.mem_len, begin + share);
-    if (split > 0 && begin >= r.mem_len) return;
+    const int begin = split * p.share, end = p.share ? min(r.mem_len, begin + p.share) : r.mem_len;
     const int row = 16 * tile + (lane & 15);
     const T* q_at = static_cast<const T*>(p.q) + ((long long)r.q_row + min(row, rows - 1) / group) * p.q_stride + (kv * group + min(row, rows - 1) % group) * p.head_dim;
     uint4 q[G::NF];
@@ -272,13 +284,13 @@ template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(
     }
     __syncthreads();
     const int in_tile = threadIdx.x / 16, chunk = threadIdx.x & 15;
-    if (splits == 1) {
+    if (!p.share) {
         finish_row<T, D>(p, r, kv, 16 * tile + in_tile, chunk, FEW_WAVES,
                          [&](int i, int what) -> const float* { return what < 2 ? &s_ml[i][what][in_tile] : &s_o[i][in_tile][NE * chunk]; });
         return;
     }
     // a part: rows of columns, then the rows' maxima and sums
-    float* part = p.parts + (size_t)blockIdx.x * part_floats(D);
+    float* part = p.parts + (size_t)id * part_floats(D);
     float top = -__builtin_inff(), sum = 0, c[NE] = {};
 #pragma unroll
     for (int i = 0; i < FEW_WAVES; ++i) top = fmaxf(top, s_ml[i][0][in_tile]);
@@ -300,17 +312,16 @@ template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(
 // A row from its parts: their maxima give each a weight, then groups of D / 4 threads take parts in turn, four columns a thread, and meet in LDS.
 constexpr int JOIN = 256;
 static_assert(MAX_SPLITS <= JOIN, "a thread for every part");
-template <typename T, int D> __global__ __launch_bounds__(JOIN) void k_cross_join(CrossArgs p, int splits, int share)
+template <typename T, int D> __global__ __launch_bounds__(JOIN) void k_cross_join(CrossArgs p)
 {
     constexpr int ACROSS = D / 4, GROUPS = JOIN / ACROSS;
     __shared__ float s_w[JOIN], s_top[JOIN / 64], s_sum[JOIN / 64];
     __shared__ float4 s_o[GROUPS][ACROSS];
-    const int id = blockIdx.x / 16, in_tile = blockIdx.x % 16, group = p.n_heads / p.n_kv_heads;
-    const CrossReq r = p.req[p.single ? id / p.n_kv_heads : request_of(p, id)];
-    const int rows = r.q_len * group, tiles = (rows + 15) / 16, kv = (id - r.first) / tiles, row = 16 * ((id - r.first) % tiles) + in_tile;
-    if (row >= rows) return;
-    const int n_parts = max(1, (r.mem_len + share - 1) / share), wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-    const float* parts = p.parts + (size_t)id * splits * part_floats(D);
+    const int group = p.n_heads / p.n_kv_heads, id = blockIdx.x;
+    const CrossReq r = p.req[request_of<&CrossReq::row>(p, id)];
+    const int rows = r.q_len * group, tiles = (rows + 15) / 16, kv = (id - r.row) / rows, row = (id - r.row) % rows, in_tile = row % 16;
+    const int n_parts = parts_of(r, p.share), wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+    const float* parts = p.parts + (size_t)(r.first + (kv * tiles + row / 16) * n_parts) * part_floats(D);
     const bool mine = (int)threadIdx.x < n_parts;
     const float* ml = parts + (size_t)(mine ? threadIdx.x : 0) * part_floats(D) + 16 * D + in_tile;
     const float m = mine ? ml[0] : -__builtin_inff(), l = mine ? ml[16] : 0.f;
@@ -618,7 +629,8 @@ template <int D, int NW, int R> hipError_t go_many(CrossArgs& a, hipStream_t s)
 template <typename T, int D, bool FULL> hipError_t go_few(CrossArgs& a, int n_cu, hipStream_t s)
 {
     int longest = 0;
-    long long wgs = 0, rows_keys = 0;                    // row tiles, and the keys that they go over
+    long long wgs = 0, rows = 0;                         // row tiles (or their parts), rows
+    double keys = 0;                                     // that all row tiles go over
     const int group = a.n_heads / a.n_kv_heads;
     a.single = true;
     for (int i = 0; i < a.n; ++i) {
@@ -626,25 +638,51 @@ template <typename T, int D, bool FULL> hipError_t go_few(CrossArgs& a, int n_cu
         a.single &= tiles == 1;
         a.req[i].first = (int)wgs;
         wgs += tiles * a.n_kv_heads;
-        rows_keys += tiles * a.n_kv_heads * a.req[i].mem_len;
+        keys += (double)tiles * a.n_kv_heads * a.req[i].mem_len;
         longest = std::max(longest, a.req[i].mem_len);
-        if (wgs > 0x7FFFFFFF) return hipErrorInvalidValue;
     }
-    // A workgroup by itself takes its memory at 50 to 100 GB/s (some 0.6 us for a step of its four waves), the join's launch costs 3 us.  So a memory is split where
-    // workgroups are few and it is long, into parts of equal length, of all requests alike, so that a round of them ends together.  us, whole / split, 8 heads of 64,
-    // bf16, requests x keys: 1 x 500 5.7 / 7.1, 1 x 1000 8.3 / 7.1, 1 x 30000 - / 17.5, 8 x 1000 8.4 / 8.6, 8 x 4000 23.7 / 18.0, 16 x 4000 24.4 / 28.4, 16 x
-    // 16000 153 / 119, 32 x 16000 209 / 231; 4 x 27000, 8 heads of 128 that four share each, 339 / 88 (5.05 TB/s).
-    const long long bytes = (long long)longest * D * sizeof(T);
-    int splits = 1, share = std::max(longest, 1);
-    if ((wgs <= n_cu / 4 && bytes >= 128 << 10) || (wgs <= n_cu / 2 && bytes >= 1 << 20)) {
-        const long long most = std::min<long long>(MAX_PARTS / wgs, MAX_SPLITS), even = rows_keys / MAX_PARTS;
-        share = (int)((std::max({even, (longest + most - 1) / most, 128LL}) + 31) / 32 * 32);
-        splits = (longest + share - 1) / share;
-        if (splits < 2) splits = 1, share = longest;
+    const bool step = a.single;
+    a.share = 0;
+    // Long memories are split, into parts of one length for all requests, where few workgroups or a few long ones would leave compute units idle.  What a compute unit has
+    // to bring of whole memories goes by latency: some 45 GB/s from the last-level cache, 22 (32 with heads of 128, whose steps are twice as large) if they come from memory;
+    // parts come at 5.1 TB/s, some of it lost, and the join costs 5 us.  us, whole / split, 8 heads of 64, bf16, requests x keys: 1 x 500 5.7 / 7.1, 1 x 1000 8.3 / 7.1, 8 x 1000 8.4 /
+    // 8.6, 8 x 4000 23.7 / 18.0, 16 x 4000 24.4 / 28.4, 24 x 16000 178 / 146, 32 x 16000 210 / 232, 40 x 16000 351 / 250, 48 x 500 .. 8000 149 /
+    // 97; 4 x 27000, 8 heads of 128 that four share each, 339 / 88 (5.05 TB/s).
+    const double row = 2.0 * a.head_dim * sizeof(T), all = keys * row, rate = all <= 256 << 20 ? 45e3 : D == 64 ? 22e3 : 32e3;
+    const double here = (longest + (double)((wgs - 1) / n_cu) * keys / wgs) * row;       // of a compute unit: the longest, and others
+    // The shortest parts that compute units hold all of at once (24 x 16000 in 960 of them 146 us, in 1152 166; 16 x 8000 with heads of 128 in 512 101, in 1024 105); shorter ones, so
+    // that it comes to even shares, where memories differ (64 x 500 .. 8000 in 1024 142, in 2048 123).
+    const bool alike = longest * (double)wgs <= 1.25 * keys;
+    const int most = std::min(MAX_PARTS, (D == 128 ? 2 : alike ? 4 : 8) * n_cu);
+    if (2 * wgs <= most && here / rate > 1.1 * all / 5.1e6 + 5) {
+        auto cut = [&](int share) {
+            long long items = 0, row = 0;
+            for (int i = 0; i < a.n; ++i) {
+                a.req[i].first = (int)items;
+                a.req[i].row = (int)row;
+                items += ((long long)a.req[i].q_len * group + 15) / 16 * a.n_kv_heads * parts_of(a.req[i], share);
+                row += (long long)a.req[i].q_len * a.n_heads;
+            }
+            return items;
+        };
+        // (memories' last parts are half as long on average; all of them whole at one and a half times this)
+        double share = std::max({keys / (most - 0.5 * wgs), (double)longest / MAX_SPLITS, 128.0});
+        while (share < longest && cut((int)std::ceil(share)) > most) share *= 1.0625;
+        if (share < longest) {
+            const int parts = (longest - 1) / (int)std::ceil(share) + 1, even = (longest - 1) / parts + 1;
+            a.share = cut(even) <= most ? even : (int)std::ceil(share);
+            wgs = cut(a.share);
+            rows = a.req[a.n - 1].row + (long long)a.req[a.n - 1].q_len * a.n_heads;
+            a.single = false;
+        }
     }
+    a.items = (int)wgs;
+    // In a step, heads of which several share a line of 128 bytes are one XCD's; others go round, which spreads long requests.  us, round / runs, 64 x 1925 keys, 4 heads that four
+    // share: heads of 40 29.0 / 15.2, of 64 23.4 / 22.1; 32 x 4000, 8 heads of 64 45 / 49; 8 x 200 .. 500 queries over 200 .. 600 keys, 8 fp32 heads of 40 39 / 45.
+    a.runs = step && a.head_dim * sizeof(T) % 128 != 0;
     const auto kernel = a.keep ? k_cross_few<T, D, FULL, true> : k_cross_few<T, D, FULL, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs * splits), dim3(FEW_WAVES * 64), 0, s, a, splits, share);
-    if (splits > 1) hipLaunchKernelGGL((k_cross_join<T, D>), dim3(16 * (unsigned)wgs), dim3(JOIN), 0, s, a, splits, share);
+    hipLaunchKernelGGL(kernel, dim3(a.runs ? (a.items + 7) / 8 * 8 : a.items), dim3(FEW_WAVES * 64), 0, s, a);
+    if (a.share) hipLaunchKernelGGL((k_cross_join<T, D>), dim3((unsigned)rows), dim3(JOIN), 0, s, a);
     return hipGetLastError();
 }
 

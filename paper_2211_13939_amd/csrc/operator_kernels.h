@@ -41,7 +41,8 @@ constexpr int CROSS_BATCH = 128;         // requests of a launch
 struct CrossReq {
     long long mem_row;
     int mem_len, q_row, q_len;
-    int first;                           // of its row tiles, of all key heads, in the launch
+    int first;                           // of its row tiles, of all key heads and as often as its memory has parts, in the launch
+    int row;                             // of its rows (query, head) in the launch, where memories have parts
 };
 struct CrossArgs {
     const void *q, *k, *v;
@@ -53,7 +54,8 @@ struct CrossArgs {
     float scale;                         // times log2(e)
     int n_heads, n_kv_heads, head_dim;
     int n;
-    bool single;                         // few rows: every request has one row tile
+    bool single, runs;                   // few rows: every request has one row tile, and no parts; an XCD takes a run of the tiles
+    int items, share;                    // few rows: tiles, and the length of a part, 0: there are none
     int start[9];                        // many rows: first of the row tiles that each XCD takes
     CrossReq req[CROSS_BATCH];
 };

@@ -143,6 +143,20 @@ def test_long_memories_in_parts(n, heads, kv, d, mem, bf16):
     _run(torch, heads, kv, d, bf16, [2] * n, _packed(lens), lens, keep=keep, seed=mem + 1)
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("n,heads,kv,d,q", [(70, 8, 4, 40, 1), (70, 4, 4, 64, 3), (90, 6, 2, 64, 12), (64, 4, 4, 128, 1), (128, 8, 8, 96, 1)])
+def test_parts_of_many_requests(n, heads, kv, d, q, bf16):
+    """A few long memories among many short ones and absent ones: requests of several row tiles, or without queries, and of as many parts as their lengths give."""
+    import torch
+    say(f"case parts {n} x {q}, {heads}/{kv} heads of {d} {'bf16' if bf16 else 'fp32'}")
+    mem = [(37 * i) % 90 for i in range(n)]
+    mem[3], mem[n - 1], mem[n // 2] = 9001, 6000, 4096
+    q_len = [(q * (i % 4 + 1)) // 2 if q > 1 else 1 for i in range(n)]
+    keep = torch.from_numpy((np.random.default_rng(n + d).random(sum(mem)) > 0.3).astype(np.uint8)).to("cuda:0")
+    for mask in (None, keep):
+        _run(torch, heads, kv, d, bf16, q_len, _packed(mem), mem, keep=mask, seed=n + q)
+
+
 @pytest.mark.parametrize("heads,kv,d,mem", [(2, 1, 64, 9000), (2, 2, 128, 8193)])
 def test_many_queries_over_long_hidden_memories(heads, kv, d, mem):
     """More than the 4096 keys whose mask is looked at at once, whole stretches hidden."""
