@@ -169,12 +169,15 @@ template <typename T, int D, bool FULL, bool MASK> struct Running {
 };
 
 // The request that tile (row) `id` of a launch is of: the last whose tiles (rows) begin at or ahead of it.
-template <int CrossReq::* FIRST = &CrossReq::first> __device__ __forceinline__ int request_of(const CrossArgs& p, int id)
+template <bool ROWS = false> __device__ __forceinline__ int request_of(const CrossArgs& p, int id)
 {
     const int lane = threadIdx.x & 63;
     int before = 0;
 #pragma unroll
-    for (int i = 0; i < CROSS_BATCH; i += 64) before += __popcll(__ballot(i + lane < p.n && p.req[min(i + lane, p.n - 1)].*FIRST <= id));
+    for (int i = 0; i < CROSS_BATCH; i += 64) {
+        const int at = min(i + lane, p.n - 1);
+        before += __popcll(__ballot(i + lane < p.n && (ROWS ? p.row[at] : p.req[at].first) <= id));
+    }
     return __builtin_amdgcn_readfirstlane(before) - 1;
 }
 
@@ -318,8 +321,9 @@ template <typename T, int D> __global__ __launch_bounds__(JOIN) void k_cross_joi
     __shared__ float s_w[JOIN], s_top[JOIN / 64], s_sum[JOIN / 64];
     __shared__ float4 s_o[GROUPS][ACROSS];
     const int group = p.n_heads / p.n_kv_heads, id = blockIdx.x;
-    const CrossReq r = p.req[request_of<&CrossReq::row>(p, id)];
-    const int rows = r.q_len * group, tiles = (rows + 15) / 16, kv = (id - r.row) / rows, row = (id - r.row) % rows, in_tile = row % 16;
+    const int at = request_of<true>(p, id), in_request = id - p.row[at];
+    const CrossReq r = p.req[at];
+    const int rows = r.q_len * group, tiles = (rows + 15) / 16, kv = in_request / rows, row = in_request % rows, in_tile = row % 16;
     const int n_parts = parts_of(r, p.share), wave = threadIdx.x / 64, lane = threadIdx.x & 63;
     const float* parts = p.parts + (size_t)(r.first + (kv * tiles + row / 16) * n_parts) * part_floats(D);
     const bool mine = (int)threadIdx.x < n_parts;
@@ -659,7 +663,7 @@ template <typename T, int D, bool FULL> hipError_t go_few(CrossArgs& a, int n_cu
             long long items = 0, row = 0;
             for (int i = 0; i < a.n; ++i) {
                 a.req[i].first = (int)items;
-                a.req[i].row = (int)row;
+                a.row[i] = (int)row;
                 items += ((long long)a.req[i].q_len * group + 15) / 16 * a.n_kv_heads * parts_of(a.req[i], share);
                 row += (long long)a.req[i].q_len * a.n_heads;
             }
@@ -672,7 +676,7 @@ template <typename T, int D, bool FULL> hipError_t go_few(CrossArgs& a, int n_cu
             const int parts = (longest - 1) / (int)std::ceil(share) + 1, even = (longest - 1) / parts + 1;
             a.share = cut(even) <= most ? even : (int)std::ceil(share);
             wgs = cut(a.share);
-            rows = a.req[a.n - 1].row + (long long)a.req[a.n - 1].q_len * a.n_heads;
+            rows = a.row[a.n - 1] + (long long)a.req[a.n - 1].q_len * a.n_heads;
             a.single = false;
         }
     }

@@ -42,7 +42,6 @@ struct CrossReq {
     long long mem_row;
     int mem_len, q_row, q_len;
     int first;                           // of its row tiles, of all key heads and as often as its memory has parts, in the launch
-    int row;                             // of its rows (query, head) in the launch, where memories have parts
 };
 struct CrossArgs {
     const void *q, *k, *v;
@@ -58,6 +57,7 @@ struct CrossArgs {
     int items, share;                    // few rows: tiles, and the length of a part, 0: there are none
     int start[9];                        // many rows: first of the row tiles that each XCD takes
     CrossReq req[CROSS_BATCH];
+    int row[CROSS_BATCH];                // few rows: first of each request's rows (query, head) in the launch, where there are parts
 };
 size_t cross_parts_bytes();
 hipError_t allow_cross();                // once on each device, before the first launch there
