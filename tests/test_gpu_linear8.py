@@ -61,6 +61,13 @@ def test_product_against_64_bits(rows, k, n, bf16):
     op.close()
 
 
+@pytest.mark.parametrize("rows,k,n", [(1100, 700, 1000), (2900, 700, 1000), (5000, 641, 999), (8300, 650, 1000), (16500, 700, 1001)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_tiles_of_each_size(rows, k, n, bf16):
+    """More than four blocks of columns: 64 x 64 to 256 x 128 tiles, whose last ones are cut in both directions."""
+    test_product_against_64_bits(rows, k, n, bf16)
+
+
 @pytest.mark.parametrize("bf16", [False, True])
 def test_rows_do_not_depend_on_their_batch(bf16):
     """What a row's neighbours are does not change it, within a form; across forms it stays within the tolerance."""
