@@ -144,7 +144,7 @@ def test_long_memories_in_parts(n, heads, kv, d, mem, bf16):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("n,heads,kv,d,q", [(70, 8, 4, 40, 1), (70, 4, 4, 64, 3), (90, 6, 2, 64, 12), (64, 4, 4, 128, 1), (128, 8, 8, 96, 1)])
+@pytest.mark.parametrize("n,heads,kv,d,q", [(70, 8, 4, 40, 1), (70, 4, 4, 64, 3), (90, 6, 2, 64, 12), (64, 4, 4, 128, 1), (128, 8, 8, 96, 1), (140, 4, 2, 64, 1)])
 def test_parts_of_many_requests(n, heads, kv, d, q, bf16):
     """A few long memories among many short ones and absent ones: requests of several row tiles, or without queries, and of as many parts as their lengths give."""
     import torch
