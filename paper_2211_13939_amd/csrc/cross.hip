@@ -169,12 +169,12 @@ template <typename T, int D, bool FULL, bool MASK> struct Running {
 };
 
 // The request that tile (row) `id` of a launch is of: the last whose tiles (rows) begin at or ahead of it.
-template <bool ROWS = false> __device__ __forceinline__ int request_of(const CrossArgs& p, int id)
+template <bool ROWS = false, typename Args> __device__ __forceinline__ int request_of(const Args& p, int id)
 {
     const int lane = threadIdx.x & 63;
     int before = 0;
 #pragma unroll
-    for (int i = 0; i < CROSS_BATCH; i += 64) {
+    for (int i = 0; i < Args::BATCH; i += 64) {
         const int at = min(i + lane, p.n - 1);
         before += __popcll(__ballot(i + lane < p.n && (ROWS ? p.row[at] : p.req[at].first) <= id));
     }
@@ -198,7 +198,7 @@ template <typename T, int NE> __device__ __forceinline__ void store_columns(T* a
 
 // The rows of a tile from the parts of its memory: maximum and sum, then columns.  `m` in units of log2; at(part) gives a part's maximum, sum and columns.
 template <typename T, int D, typename At>
-__device__ __forceinline__ void finish_row(const CrossArgs& p, const CrossReq& r, int kv, int row, int chunk, int n_parts, At at)
+__device__ __forceinline__ void finish_row(const CrossCommon& p, const CrossReq& r, int kv, int row, int chunk, int n_parts, At at)
 {
     constexpr int NE = D / 16;
     const int group = p.n_heads / p.n_kv_heads;
@@ -223,7 +223,7 @@ __device__ __forceinline__ void finish_row(const CrossArgs& p, const CrossReq& r
 }
 
 // A tile of 16 rows over a part of its request's memory; the waves take steps of keys in turn, the next one's on its way, and meet in LDS.
-template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(FEW_WAVES * 64) void k_cross_few(CrossArgs p)
+template <typename T, int D, bool FULL, bool MASK, typename Args> __global__ __launch_bounds__(FEW_WAVES * 64) void k_cross_few(Args p)
 {
     using G = Geometry<T, D>;
     constexpr int NE = G::NE, PITCH = D + 4, STRIDE = FEW_WAVES * G::N;
@@ -315,7 +315,7 @@ template <typename T, int D, bool FULL, bool MASK> __global__ __launch_bounds__(
 // A row from its parts: their maxima give each a weight, then groups of D / 4 threads take parts in turn, four columns a thread, and meet in LDS.
 constexpr int JOIN = 256;
 static_assert(MAX_SPLITS <= JOIN, "a thread for every part");
-template <typename T, int D> __global__ __launch_bounds__(JOIN) void k_cross_join(CrossArgs p)
+template <typename T, int D, typename Args> __global__ __launch_bounds__(JOIN) void k_cross_join(Args p)
 {
     constexpr int ACROSS = D / 4, GROUPS = JOIN / ACROSS;
     __shared__ float s_w[JOIN], s_top[JOIN / 64], s_sum[JOIN / 64];
@@ -684,10 +684,19 @@ template <typename T, int D, bool FULL> hipError_t go_few(CrossArgs& a, int n_cu
     // In a step, heads of which several share a line of 128 bytes are one XCD's; others go round, which spreads long requests.  us, round / runs, 64 x 1925 keys, 4 heads that four
     // share: heads of 40 29.0 / 15.2, of 64 23.4 / 22.1; 32 x 4000, 8 heads of 64 45 / 49; 8 x 200 .. 500 queries over 200 .. 600 keys, 8 fp32 heads of 40 39 / 45.
     a.runs = step && a.head_dim * sizeof(T) % 128 != 0;
-    const auto kernel = a.keep ? k_cross_few<T, D, FULL, true> : k_cross_few<T, D, FULL, false>;
-    hipLaunchKernelGGL(kernel, dim3(a.runs ? (a.items + 7) / 8 * 8 : a.items), dim3(FEW_WAVES * 64), 0, s, a);
-    if (a.share) hipLaunchKernelGGL((k_cross_join<T, D>), dim3((unsigned)rows), dim3(JOIN), 0, s, a);
-    return hipGetLastError();
+    auto launch = [&](const auto& args) {
+        using Args = std::decay_t<decltype(args)>;
+        const auto kernel = a.keep ? k_cross_few<T, D, FULL, true, Args> : k_cross_few<T, D, FULL, false, Args>;
+        hipLaunchKernelGGL(kernel, dim3(a.runs ? (a.items + 7) / 8 * 8 : a.items), dim3(FEW_WAVES * 64), 0, s, args);
+        if (a.share) hipLaunchKernelGGL((k_cross_join<T, D, Args>), dim3((unsigned)rows), dim3(JOIN), 0, s, args);
+        return hipGetLastError();
+    };
+    if (a.n > CROSS_SMALL) return launch(a);
+    CrossArgsOf<CROSS_SMALL> small;
+    static_cast<CrossCommon&>(small) = a;
+    std::copy_n(a.req, a.n, small.req);
+    if (a.share) std::copy_n(a.row, a.n, small.row);
+    return launch(small);
 }
 
 }  // namespace

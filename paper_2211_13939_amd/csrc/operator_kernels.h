@@ -43,7 +43,7 @@ struct CrossReq {
     int mem_len, q_row, q_len;
     int first;                           // of its row tiles, of all key heads and as often as its memory has parts, in the launch
 };
-struct CrossArgs {
+struct CrossCommon {
     const void *q, *k, *v;
     void* out;
     const uint8_t* keep;
@@ -56,9 +56,15 @@ struct CrossArgs {
     bool single, runs;                   // few rows: every request has one row tile, and no parts; an XCD takes a run of the tiles
     int items, share;                    // few rows: tiles, and the length of a part, 0: there are none
     int start[9];                        // many rows: first of the row tiles that each XCD takes
-    CrossReq req[CROSS_BATCH];
-    int row[CROSS_BATCH];                // few rows: first of each request's rows (query, head) in the launch, where there are parts
 };
+template <int N> struct CrossArgsOf : CrossCommon {
+    static constexpr int BATCH = N;
+    CrossReq req[N];
+    int row[N];                          // few rows: first of each request's rows (query, head) in the launch, where there are parts
+};
+using CrossArgs = CrossArgsOf<CROSS_BATCH>;
+// Small batches of few rows take small arguments: what a launch carries costs the host (a request's step from Python 6.8 us with 3.7 KB, 5.6 with 0.6).
+constexpr int CROSS_SMALL = 16;
 size_t cross_parts_bytes();
 hipError_t allow_cross();                // once on each device, before the first launch there
 // `few`: 16 rows a workgroup, both types; `many`: 128 or 256, two bytes alone.  They fill in what the launch's tiles are.
