@@ -193,6 +193,13 @@ template <typename XT, typename RT, int LPR, int NC> __global__ __launch_bounds_
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int i = 0; i < 8; ++i) t[c][i] = t[c][i] * inv * g[c][i];
+        // 0 times an infinity or a NaN (a row with a NaN in it, or of zeros without an eps) is NaN, and what lies past dim stays zero.
+        if (!(inv < __builtin_inff())) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[c][i] = (c * LPR + lane) * 8 + i < p.dim ? t[c][i] : 0.f;
+        }
     }
     if (p.y) {
 #pragma unroll

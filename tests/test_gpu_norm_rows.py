@@ -1,0 +1,55 @@
+"""tts_norm's rows that are no ordinary numbers: what a NaN, an infinity, zeros without an eps come to, in their own row, in the columns past its end and in the rows beside
+it."""
+import numpy as np
+import pytest
+
+from paper_2211_13939_amd import binding
+from tests import operator_ref as ref
+from tests.helpers import say
+
+pytestmark = pytest.mark.gpu
+
+
+def _run(torch, x, gain, eps):
+    rows, dim = x.shape
+    op = binding.Norm(binding.make_norm_config(dim, eps=eps), gain, stream=torch.cuda.current_stream())
+    y = torch.full((rows, dim), 7.0, device="cuda:0")
+    b = torch.empty(rows, binding.width8(dim), dtype=torch.float8_e4m3fn, device="cuda:0")
+    s = torch.empty(rows, binding.scale_columns(dim), dtype=torch.float8_e8m0fnu, device="cuda:0")
+    b.view(torch.uint8).fill_(0x55)
+    s.view(torch.uint8).fill_(0x55)
+    op.run_device(torch.from_numpy(x).to("cuda:0"), y=y, y8=b, scales=s)
+    torch.cuda.synchronize()
+    op.close()
+    return y.cpu().numpy(), b.view(torch.uint8).cpu().numpy(), s.view(torch.uint8).cpu().numpy()
+
+
+# a wave's rows of one, two and four chunks a lane; a workgroup's of one, two, four and eight
+SHAPES = [(5, 100), (2100, 700), (2100, 1500), (6, 700), (5, 2049), (4, 4200), (4, 16001)]
+
+
+@pytest.mark.parametrize("rows,dim", SHAPES)
+def test_columns_past_the_end_are_zeros_whatever_the_row_holds(rows, dim):
+    import torch
+    say(f"case odd rows {rows} x {dim}")
+    rng = np.random.default_rng(dim)
+    gain = (1 + 0.2 * rng.standard_normal(dim)).astype(np.float32)
+    x = rng.standard_normal((rows, dim)).astype(np.float32)
+    _, plain_b, plain_s = _run(torch, x, gain, 0.0)
+    odd = x.copy()
+    odd[0, dim // 2] = np.nan
+    odd[1, dim - 1], odd[1, 3] = np.inf, -np.inf
+    odd[2] = 0
+    y, b, s = _run(torch, odd, gain, 0.0)
+    n = ref.blocks_of(dim)
+    assert (b[:, dim:] == 0).all() and (s[:, n:] == 127).all()
+    assert np.isnan(y[0]).all() and ((b[0, :dim] & 127) == 127).all() and (s[0] == 127).all()
+    # divided by an infinity: zeros, and NaN where the infinities are
+    there = np.isinf(odd[1])
+    assert np.isnan(y[1][there]).all() and (y[1][~there] == 0).all() and ((b[1, :dim][there] & 127) == 127).all() and ((b[1, :dim][~there] & 127) == 0).all() and (s[1] == 127).all()
+    assert np.isnan(y[2]).all() and ((b[2, :dim] & 127) == 127).all()          # 0 / 0
+    np.testing.assert_array_equal(b[3:], plain_b[3:])
+    np.testing.assert_array_equal(s[3:], plain_s[3:])
+    # with an eps zeros are zeros
+    y, b, s = _run(torch, odd, gain, 1e-5)
+    assert (y[2] == 0).all() and (b[2, :dim] & 127 == 0).all() and (s[2] == 127).all() and (b[:, dim:] == 0).all()
