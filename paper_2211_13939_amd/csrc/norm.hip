@@ -176,19 +176,36 @@ template <typename XT, typename RT, int LPR, int NC> __global__ __launch_bounds_
     }
     if (!p.y && !p.y8) return;
     if (p.gain) {
-        float sum = 0;
+        // (the mean of the squares of a row times `by`)
+        auto mean_square = [&](float by) {
+            float sum = 0;
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+            for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += t[c][i] * t[c][i];
-        sum = row16_sum(sum);
-        sum = (lane_value(sum, 0) + lane_value(sum, 16)) + (lane_value(sum, 32) + lane_value(sum, 48));
-        if constexpr (LPR > 64) {
-            if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = sum;
-            __syncthreads();
-            sum = (part[0] + part[1]) + (part[2] + part[3]);
+                for (int i = 0; i < 8; ++i) sum += (t[c][i] * by) * (t[c][i] * by);
+            sum = row16_sum(sum);
+            sum = (lane_value(sum, 0) + lane_value(sum, 16)) + (lane_value(sum, 32) + lane_value(sum, 48));
+            if constexpr (LPR > 64) {
+                if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = sum;
+                __syncthreads();
+                sum = (part[0] + part[1]) + (part[2] + part[3]);
+            }
+            return sum / p.dim;
+        };
+        const float mean = mean_square(1.0f) + p.eps;
+        float inv = 1.0f / sqrtf(mean);
+        if (!(mean >= 0x1p-100f && mean < __builtin_inff())) {
+            // Squares that leave fp32's range: the row times a power of two has the same quotient, its squares' sum another that is undone.  (Elements lie below 2^-43 in the first case.  In the second most
+            // of the factor is the sum's alone, small ones beside large ones would lose bits to it.)
+            const bool small = mean < 0x1p-100f;
+            const float row_by = small ? 0x1p100f : 0x1p-4f, sum_by = small ? 1.0f : 0x1p-76f, by = row_by * sum_by;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[c][i] *= row_by;
+            if constexpr (LPR > 64) __syncthreads();      // (the first sum is read)
+            inv = sum_by / sqrtf(mean_square(sum_by) + p.eps * by * by);
         }
-        const float inv = 1.0f / sqrtf(sum / p.dim + p.eps);
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll

@@ -1,11 +1,12 @@
-"""tts_norm's rows that are no ordinary numbers: what a NaN, an infinity, zeros without an eps come to, in their own row, in the columns past its end and in the rows beside
-it."""
+"""tts_norm's rows that are no ordinary numbers: what a NaN, an infinity, zeros without an eps or magnitudes whose squares leave fp32's range come to, in their own row, in
+the columns past its end and in the rows beside it."""
 import numpy as np
 import pytest
 
 from paper_2211_13939_amd import binding
 from tests import operator_ref as ref
 from tests.helpers import say
+from tests.test_gpu_norm import _check_8, _tolerance
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +54,33 @@ def test_columns_past_the_end_are_zeros_whatever_the_row_holds(rows, dim):
     # with an eps zeros are zeros
     y, b, s = _run(torch, odd, gain, 1e-5)
     assert (y[2] == 0).all() and (b[2, :dim] & 127 == 0).all() and (s[2] == 127).all() and (b[:, dim:] == 0).all()
+
+
+@pytest.mark.parametrize("rows,dim", [(40, 100), (2100, 700), (2100, 1500), (40, 700), (40, 2049), (40, 4200), (40, 16001)])
+@pytest.mark.parametrize("eps", [0.0, 1e-36, 1e-5, 1e30, 3e38])
+def test_rows_whose_squares_leave_the_range_of_fp32(rows, dim, eps):
+    """Magnitudes from the least to the largest of fp32, in rows of their own and small ones among large: y is the definition's to the same tolerance.  (Results below 2^-126 are
+    multiples of 2^-149: one step each, of the quotient and of its product with the gain.)"""
+    import torch
+    say(f"case rows of any size {rows} x {dim} eps {eps}")
+    rng = np.random.default_rng(dim)
+    gain = (1 + 0.2 * rng.standard_normal(dim)).astype(np.float32)
+    v = rng.uniform(0.5, 1.0, (rows, dim)) * rng.choice([-1.0, 1.0], (rows, dim))
+    e = np.resize([-148, -140, -126, -101, -75, -64, -63, -52, -50, -49, -30, 0, 30, 56, 57, 60, 63, 64, 65, 80, 100, 120, 127, 128], rows)
+    v = v * 2.0 ** e[:, None]
+    v[rows // 2:, ::3] *= 2.0 ** -60
+    x = v.astype(np.float32)
+    y, b, s = _run(torch, x, gain, eps)
+    with np.errstate(invalid="ignore"):
+        _, want = ref.norm(x, None, gain, np.float32(eps))
+    none = ~x.any(1)
+    if eps == 0:
+        assert np.isnan(y[none]).all()
+    else:
+        assert (y[none] == 0).all()
+    y, want, b, s = y[~none].astype(np.float64), want[~none], b[~none], s[~none]
+    tol = _tolerance(dim)
+    assert (np.abs(y - want) <= tol * np.abs(want) + 2.0 ** -149 * (1 + np.abs(gain))).all()
+    # 8-bit rows, of values that are no smaller than fp32's normal ones
+    sure = (np.abs(want).max(1) > 2.0 ** -100) | (want == 0).all(1)
+    _check_8(torch.from_numpy(b[sure]).view(torch.float8_e4m3fn), torch.from_numpy(s[sure]).view(torch.float8_e8m0fnu), want[sure], dim, tol)
