@@ -9,8 +9,10 @@
  * channel.  The products of e4m3 numbers are summed by the matrix instructions, which apply the scales themselves.
  *
  * With y in bf16 the sums are the 8-bit instructions' (fp32 results; within an instruction of 128 columns, terms are
- * aligned to the largest: an error of some 1.4e-5 of the result, where bf16 carries 2^-9).  With y in fp32 the operands are
- * brought to bf16, which holds every e4m3 number times its scale exactly, and the sums are fp32 throughout, at up to half the rate.
+ * aligned to the largest: an error of some 1.4e-5 of the result, where bf16's rounding is up to 2^-8).  With y in fp32 the operands are
+ * brought to bf16 together with their scales, and the sums are fp32 throughout, at up to half the rate.  bf16 holds every e4m3 number times
+ * a scale from 2^-124 to 2^119 exactly.  In blocks whose largest magnitude is at most 448 * 2^-125, of either operand, it rounds operands to multiples
+ * of 2^-133; in those where it is above 448 * 2^119 (2.98e38) numbers of 256 * 2^120 and more become infinite.  bf16 results know no such limits.
  *
  * Everything is queued on the stream given at creation; device memory comes from the caller's arena; nothing is
  * allocated on the device.  A call is one launch and may be captured into a graph.

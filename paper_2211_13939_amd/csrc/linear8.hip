@@ -19,7 +19,7 @@ __device__ __forceinline__ intx8 operand(const Frag8& f) { return __builtin_bit_
 
 // Two forms of the sums.  Fast: the 8-bit instruction's own.  It aligns the products of an instruction to the largest and drops bits some 2^-17 below it, 1.4e-5
 // of the result for normal values, far below a bf16 result's rounding.  Exact: operands brought to bf16 with their scales (e4m3's four bits and
-// any power of two fit), four instructions of 32 columns: 4e-8 to 8e-8.
+// a power of two from 2^-124 to 2^119 fit; of smaller ones bf16's least number, 2^-133, cuts bits off, and 256 * 2^120 is no bf16 number), four instructions of 32 columns: 4e-8 to 8e-8.
 template <bool EXACT> struct Operand;
 template <> struct Operand<false> {
     Frag8 f;
@@ -32,7 +32,7 @@ template <> struct Operand<true> {
     Operand() = default;
     __device__ __forceinline__ Operand(const Frag8& v, uint32_t byte)
     {
-        const float by = __uint_as_float(byte << 23);
+        const float by = __uint_as_float(byte << 23);     // (the conversion takes its exponent's field alone: 0 is 2^-127 to it)
         const intx8 w = operand(v);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
