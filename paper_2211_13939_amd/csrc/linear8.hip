@@ -472,39 +472,18 @@ template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS> hipEr
 
 template <typename YT> hipError_t go(const Linear8Args& a, int n_cu, hipStream_t s)
 {
-    const int units = channel_units(a.out_dim);
-    // A few rows: memory's rate is what counts (8192 x 8192 weights 11.6 us, 5.8 TB/s).  Up to 16 of them the plain loads of x still cost less than
-    // a ring, unless the weights are many (16 rows, k_linear8_few / k_linear8_split: 1024 x 1024 2.8 / 3.2 us, 4096 x 4096 5.7 / 5.2, 8192 x 8192 15.7 /
-    // 12.3; 8 rows of 4096 x 4096 4.5 / 5.0).
-    if (a.rows <= 8 || (a.rows <= 16 && units * a.blocks <= 2048)) {
-        hipLaunchKernelGGL((k_linear8_few<YT>), dim3(2 * units), dim3(FEW_WAVES * 64), 0, s, a);
+    constexpr bool TWO = sizeof(YT) == 2;
+    switch (linear8_form(a.rows, a.out_dim, a.blocks, TWO, n_cu)) {
+    case Linear8Form::FEW:
+        hipLaunchKernelGGL((k_linear8_few<YT>), dim3(2 * channel_units(a.out_dim)), dim3(FEW_WAVES * 64), 0, s, a);
         return hipGetLastError();
+    case Linear8Form::SPLIT: return go_split<YT, 1, 2>(a, s);
+    case Linear8Form::TILE_64_64: return go_many<YT, 1, 1, 2, 2, 2, TWO ? 3 : 2>(a, s);
+    case Linear8Form::TILE_64_128: return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
+    case Linear8Form::TILE_128_128: return go_many<YT, 2, 2, 2, 2, 2, 2>(a, s);
+    case Linear8Form::TILE_256_128: break;
     }
-    // Otherwise tiles: a larger one asks for fewer bytes, a smaller one has its latencies spread over more workgroups.  us, two-byte results, 32 x 32 split / 64 x 64 / 64
-    // channels x 128 rows / 128 x 128 / 256 x 128: 200 x 2048 x 2048 5.7 / 6.6 / 8.3 / 12.3 / 20.6; 512 x 2048 x 2048 10.0 / 6.9 / 8.4 / 12.5 / 20.7; 1024 x 2048 x 2048 17.0 / 8.4 /
-    // 9.2 / 12.5 / 20.9; 1542 x 2048 x 2048 - / 15.6 / 11.5 / 13.6 / 21.2; 3500 x 2048 x 2048 - / 25.7 / 25.6 / 19.5 / 22.9; 8000 x 1024 x 1024 - / 16.3 / 15.1 / 13.1 / 16.0; 16384 x
-    // 1024 x 1024 - / 33.0 / 27.1 / 27.4 / 24.9; 16384 x 4096 x 4096 - / 427 / 358 / 278 / 251.
-    auto tiles = [&](int n, int m) { return (long long)((units + n - 1) / n) * ((a.rows + 32 * m - 1) / (32 * m)); };
-    const int two = 2 * n_cu;
-    if (tiles(1, 1) <= two) return go_split<YT, 1, 2>(a, s);
-    // (few columns: a workgroup is its first loads and its results, of which more, smaller ones have more at once.  64 x 128 rows against the largest: 16384 x 512 x 2048 32.0 /
-    // 35.5 us, 4096 x 256 x 1024 5.2 / 6.5; 16384 x 640 x 2048 38.6 / 34.9.)
-    if (a.blocks <= 4 && tiles(2, 4) >= two) return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
-    if constexpr (sizeof(YT) == 2) {
-        // The smallest that goes round once with two workgroups a compute unit: what comes in a second round costs a whole one.
-        if (tiles(2, 2) <= two) return go_many<YT, 1, 1, 2, 2, 2, 3>(a, s);
-        if (tiles(2, 4) <= two) return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
-        if (tiles(4, 4) <= two) return go_many<YT, 2, 2, 2, 2, 2, 2>(a, s);
-        return go_many<YT, 4, 2, 2, 2, 1, 3>(a, s);
-    } else {
-        // Operands' way to bf16 keeps the vector pipes busy, and several workgroups a compute unit even out.  The largest that leaves two of them: us, 64 x 64 / 64 x 128 / 128 x
-        // 128 / 256 x 128: 1280 x 2048 x 2048 17.5 / 18.6 / 19.9 / 33.7, 3000 x 2048 x 2048 32.9 / 30.5 / 31.9 / 35.4, 3000 x 4096 x 4096 115 / 102 / 94 / 102, 16384 x 4096 x
-        // 4096 657 / 550 / - / 460.  (64 x 64 with two steps in LDS, four workgroups a compute unit: 1542 x 2048 x 2048 23.8 -> 21.7.)
-        if (tiles(8, 4) >= two) return go_many<YT, 4, 2, 2, 2, 1, 3>(a, s);
-        if (tiles(4, 4) >= two) return go_many<YT, 2, 2, 2, 2, 2, 2>(a, s);
-        if (tiles(2, 4) >= two) return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
-        return go_many<YT, 1, 1, 2, 2, 2, 2>(a, s);
-    }
+    return go_many<YT, 4, 2, 2, 2, 1, 3>(a, s);
 }
 
 }  // namespace

@@ -1,17 +1,18 @@
-"""tts_linear8 in each of its forms: scales over all of their range and in more words than one."""
+"""tts_linear8 in each of its forms: scales over all of their range and in more words than one, blocks of zeros, a NaN's row, rows around the array, replays of a graph."""
 import numpy as np
 import pytest
 
 from paper_2211_13939_amd import binding
 from tests import operator_ref as ref
 from tests.helpers import say
-from tests.test_gpu_linear8 import _want
+from tests.test_gpu_linear8 import _rows8, _want
 
 pytestmark = pytest.mark.gpu
 
-# (rows, in_dim, out_dim) by the form that a device of 256 compute units takes for bf16 and for fp32 results
+# (rows, in_dim, out_dim) by the form that a device of 256 compute units takes for bf16 and for fp32 results (tests/test_operator_plans.py asks the rule)
 SHAPES = {(5, 1300, 100): ("few", "few"), (50, 1300, 100): ("split", "split"), (2100, 200, 2050): ("64x128", "64x128"), (1100, 1300, 1000): ("64x64", "64x64"),
           (2900, 641, 1000): ("64x128", "64x64"), (5000, 641, 999): ("128x128", "64x128"), (8300, 641, 1000): ("256x128", "128x128"), (16500, 641, 1001): ("256x128", "256x128")}
+LARGE = [s for s in SHAPES if s[0] > 1000]
 
 
 def _wide(rng, rows, k, n, least, most):
@@ -82,3 +83,56 @@ def test_every_number_at_the_ends_of_the_scales(rows, n, bf16):
             x = np.round(x * 2.0 ** 133) * 2.0 ** -133
         want = np.tile(x * 2.0 ** e, (1, n // 128))
         np.testing.assert_array_equal(_call(torch, c, sx, w, None, bf16), want, err_msg=str(byte))
+
+
+@pytest.mark.parametrize("rows,k,n", LARGE)
+@pytest.mark.parametrize("bf16", [False, True])
+def test_zero_blocks_and_a_nan_in_large_calls(rows, k, n, bf16):
+    import torch
+    rng = np.random.default_rng(k)
+    x = rng.standard_normal((rows, k)) * np.exp(rng.standard_normal((rows, 1)))
+    x[:, 128:256] = 0
+    x[7] = 0
+    w = (rng.standard_normal((n, k)) / np.sqrt(k)).astype(np.float32)
+    w[:, k // 128 * 128:] = 0
+    w[5] = 0
+    codes, sx = ref.round8(x)
+    bad = [0, rows // 2, rows - 1]
+    where = (codes[bad, 77].copy(), codes[bad, k - 1].copy())
+    want, tol = _want(codes, sx, w, None, bf16)
+    codes[bad[0], 77] = codes[bad[1], k - 1] = 0x7F
+    codes[bad[2], 77] = 0xFF
+    got = _call(torch, codes, sx, w, None, bf16)
+    assert np.isnan(got[bad]).all()
+    rest = np.setdiff1d(np.arange(rows), bad)
+    assert (np.abs(got[rest] - want[rest]) <= tol[rest]).all() and (got[7] == 0).all() and (got[rest, 5] == 0).all()
+
+
+@pytest.mark.parametrize("rows,k,n", [(2100, 200, 2050), (1100, 1300, 1000), (5000, 641, 999), (8300, 641, 1000)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_a_graph_of_a_large_call(rows, k, n, bf16):
+    import torch
+    rng = np.random.default_rng(3)
+    w = rng.standard_normal((n, k)).astype(np.float32)
+    op = binding.Linear8(binding.make_linear8_config(k, n, bf16), w)
+    made = [_rows8(torch, rng.standard_normal((rows, k)))[2:] for _ in range(3)]
+    x8, sx = (t.clone() for t in made[0])
+    y = torch.empty(rows, n, dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda:0")
+    op.run_device(x8, sx, y)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=op.stream):
+        op.run_device(x8, sx, y)
+    for i, (a, b) in enumerate(made + made[:1]):
+        x8.view(torch.uint8).copy_(a.view(torch.uint8))
+        sx.view(torch.uint8).copy_(b.view(torch.uint8))
+        y.fill_(5)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(op.stream):
+            g.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        op.run_device(x8, sx, y)
+        torch.cuda.synchronize()
+        assert torch.equal(got, y), i
+    op.close()
