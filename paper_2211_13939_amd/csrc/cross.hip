@@ -723,16 +723,7 @@ hipError_t launch_cross_few(CrossArgs& a, bool bf16, int n_cu, hipStream_t s)
 
 hipError_t launch_cross_many(CrossArgs& a, int n_cu, hipStream_t s)
 {
-    // 256 rows a workgroup where memories are long and it leaves some for most compute units, 128 otherwise.  us, 128 / 256: 8 requests of 3000 queries over
-    // 3000 keys, 16 heads of 64 356 / 325, 16 of 128 that share 4 620 / 560; one of 4000 over 4000 (252 workgroups) 143 / 134, of 1000 over 1000 24 / 31;
-    // 64 of 600 over 135 33 / 35.
-    long long large = 0;
-    int longest = 0;
-    for (int i = 0; i < a.n; ++i) {
-        large += ((long long)a.req[i].q_len * (a.n_heads / a.n_kv_heads) + 255) / 256 * a.n_kv_heads;
-        longest = std::max(longest, a.req[i].mem_len);
-    }
-    const bool eight = longest >= 1024 && large >= n_cu - n_cu / 4;
+    const bool eight = cross_many_large(a.req, a.n, a.n_heads / a.n_kv_heads, a.n_kv_heads, n_cu);
     if (a.head_dim > 64) return eight ? go_many<128, 8, 3>(a, s) : go_many<128, 4, 2>(a, s);
     return eight ? go_many<64, 8, 3>(a, s) : go_many<64, 4, 3>(a, s);
 }

@@ -110,5 +110,18 @@ hipError_t launch_cross_many(CrossArgs& a, int n_cu, hipStream_t s);
 constexpr int CROSS_MANY_ROWS = 33;
 constexpr int CROSS_MAX_TILES = 1 << 23;     // a grid has fewer than 2^32 threads, and XCDs' shares of the tiles may be of different heights
 inline bool cross_many(long long few_tiles, int n_cu) { return 2 * few_tiles >= 5LL * n_cu; }
+// 256 rows a workgroup where memories are long and it leaves some for most compute units, 128 otherwise.  us, 128 / 256: 8 requests of 3000 queries over
+// 3000 keys, 16 heads of 64 356 / 325, 16 of 128 that share 4 620 / 560; one of 4000 over 4000 (252 workgroups) 143 / 134, of 1000 over 1000 24 / 31;
+// 64 of 600 over 135 33 / 35.
+inline bool cross_many_large(const CrossReq* req, int n, int group, int n_kv_heads, int n_cu)
+{
+    long long large = 0;
+    int longest = 0;
+    for (int i = 0; i < n; ++i) {
+        large += ((long long)req[i].q_len * group + 255) / 256 * n_kv_heads;
+        longest = req[i].mem_len > longest ? req[i].mem_len : longest;
+    }
+    return longest >= 1024 && large >= n_cu - n_cu / 4;
+}
 
 }  // namespace tts
