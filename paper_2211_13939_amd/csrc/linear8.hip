@@ -338,12 +338,11 @@ template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS> struc
 };
 
 template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS>
-__global__ __launch_bounds__(64 * WN * WM, WN * WM / 4) void k_linear8_many(Linear8Args p, int n_tiles, int m_tiles)
+__global__ __launch_bounds__(64 * WN * WM, WN * WM / 4) void k_linear8_many(Linear8Args p, int n_tiles, int m_tiles, int across)
 {
     extern __shared__ __align__(16) uint8_t lds[];
-    // Workgroups are dealt to the eight XCDs in turn; an XCD takes a run of tiles, 4 rows of tiles high, so that its L2 holds what they share.
-    const int total = n_tiles * m_tiles, per = (total + 7) / 8;
-    const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    // An XCD's run of tiles is 4 rows of tiles high, so that its L2 holds what they share.
+    const int total = n_tiles * m_tiles, id = linear8_tile(blockIdx.y * across + blockIdx.x, total);
     if (id >= total) return;
     const int band = id / (4 * n_tiles), in_band = id - band * 4 * n_tiles, high = min(4, m_tiles - 4 * band);
     Many<YT, TN, TM, WN, WM, SUB, STEPS> many(p, lds, in_band / high, 4 * band + in_band % high);
@@ -466,7 +465,8 @@ template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS> hipEr
 {
     using M = Many<YT, TN, TM, WN, WM, SUB, STEPS>;
     const int n_tiles = (channel_units(a.out_dim) + M::NT - 1) / M::NT, m_tiles = (a.rows + M::MT * 32 - 1) / (M::MT * 32);
-    hipLaunchKernelGGL((k_linear8_many<YT, TN, TM, WN, WM, SUB, STEPS>), dim3((n_tiles * m_tiles + 7) / 8 * 8), dim3(64 * WN * WM), M::LDS, s, a, n_tiles, m_tiles);
+    const Linear8Grid grid = linear8_grid(n_tiles * m_tiles);
+    hipLaunchKernelGGL((k_linear8_many<YT, TN, TM, WN, WM, SUB, STEPS>), dim3(grid.across, grid.down), dim3(64 * WN * WM), M::LDS, s, a, n_tiles, m_tiles, grid.across);
     return hipGetLastError();
 }
 

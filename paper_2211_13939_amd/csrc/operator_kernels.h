@@ -25,6 +25,20 @@ hipError_t launch_norm(const NormArgs& a, bool x_bf16, bool res_bf16, int n_cu, 
 constexpr int channel_units(int channels) { return (channels + 63) / 64 * 2; }
 constexpr int channel_unit(int n) { return n / 64 * 2 + n / 16 % 2; }
 constexpr int channel_row(int n) { return n / 4 % 4 * 8 + n / 32 % 2 * 4 + n % 4; }
+// A launch of `tiles` workgroups, which eight XCDs are dealt in turn: an XCD takes a run of tiles.  A side of a grid has fewer than 2^32 threads, so that large calls' lie on two, rows of
+// them a multiple of eight wide.  (Some workgroups are left over: linear8_tile is `tiles` or more for them.)
+struct Linear8Grid { int across, down; };
+inline Linear8Grid linear8_grid(int tiles)
+{
+    const int wgs = (tiles + 7) / 8 * 8, down = (wgs - 1) / (1 << 20) + 1;
+    return {((wgs + down - 1) / down + 7) / 8 * 8, down};
+}
+__host__ __device__ inline int linear8_tile(int wg, int tiles)
+{
+    const int per = (tiles + 7) / 8, at = wg >> 3;
+    return at < per ? (wg & 7) * per + at : tiles;
+}
+
 struct Linear8Args {
     const uint8_t *x8, *sx;              // [rows][width8], [rows][scale_columns]
     const uint4* w;                      // [units][halves of blocks][2][64 lanes] 16 bytes: the c-th of lane l holds row l % 32 of the unit, columns 32 * (l / 32) + 16 * c ..

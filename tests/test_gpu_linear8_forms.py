@@ -136,3 +136,26 @@ def test_a_graph_of_a_large_call(rows, k, n, bf16):
         torch.cuda.synchronize()
         assert torch.equal(got, y), i
     op.close()
+
+
+def test_more_tiles_than_a_row_of_the_grid_has():
+    """2^20 of them and some, of as many rows as a call may have."""
+    import torch
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("22 GB")
+    rows, k, n = 1 << 24, 128, 513
+    rng = np.random.default_rng(5)
+    w = (rng.standard_normal((n, k)) / np.sqrt(k)).astype(np.float32)
+    at = [0, 1, 127, 128, (1 << 23) - 1, 1 << 23, (1 << 23) + 1, 10000019, rows - 1]
+    codes, sx = ref.round8(rng.standard_normal((len(at), k)))
+    want, tol = _want(codes, sx, w, None, True)
+    x8, scales = torch.zeros(rows, k, dtype=torch.uint8, device="cuda:0"), torch.full((rows, 4), 127, dtype=torch.uint8, device="cuda:0")
+    x8[at], scales[at] = torch.from_numpy(codes).to("cuda:0"), torch.from_numpy(sx).to("cuda:0")
+    y = torch.full((rows, n), 9.0, dtype=torch.bfloat16, device="cuda:0")
+    op = binding.Linear8(binding.make_linear8_config(k, n, True), w, stream=torch.cuda.current_stream())
+    op.run_device(x8.view(torch.float8_e4m3fn), scales.view(torch.float8_e8m0fnu), y)
+    torch.cuda.synchronize()
+    assert (np.abs(y[at].double().cpu().numpy() - want) <= tol).all()
+    y[at] = 0
+    assert not any(bool(part.any()) for part in y.split(1 << 20))
+    op.close()

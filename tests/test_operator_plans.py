@@ -38,6 +38,15 @@ def test_every_form_of_the_product_has_its_shapes(plans):
         assert {FORMS[plans.plan_linear8(*s, 1 - i, N_CU)] for s in test_gpu_linear8_forms.LARGE} == set(FORMS[2:])
 
 
+@pytest.mark.parametrize("tiles", [1, 7, 8, 9, 1000, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, (1 << 20) + 9, 3 * (1 << 20) + 5, (1 << 24) - 3, 1 << 24, (1 << 25) + 13, 1 << 28])
+def test_the_products_grid_has_a_workgroup_for_every_tile(plans, tiles):
+    """Up to 2^24 rows and 65536 channels in tiles of 64 x 64: each side of the grid is one that can be launched, and workgroups of a row of it stay in turn with the XCDs."""
+    across, down = C.c_int(), C.c_int()
+    assert plans.plan_linear8_grid(tiles, C.byref(across), C.byref(down)) == 0
+    assert across.value % 8 == 0 and across.value * 256 < 1 << 32 and down.value < 1 << 16
+    assert across.value * down.value < tiles + 8 * down.value + 8
+
+
 def _launches(lib, heads, kv, d, q_len, mem):      # noqa: F811
     """(launches, those for many queries, requests in all of them) of a call of the library's host code."""
     lib.fake_reset()
