@@ -390,10 +390,10 @@ template <int N> __device__ __forceinline__ void arrived()
     static_assert(N < 64, "the counter has six bits");
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
-// (written out as in linear8.hip: no registers to come back to, m0 has no other user)
+// (written out as in linear8.hip: no registers to come back to)
 __device__ __forceinline__ void to_lds(const char* from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
 }
 
 // (128 registers where heads are narrow and tiles large: with 135 of them 3 waves in place of 4 share a SIMD, and 16 heads of 3000 x 3000 x 64 in eight requests
