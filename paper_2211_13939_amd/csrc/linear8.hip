@@ -139,8 +139,8 @@ template <typename YT> __global__ __launch_bounds__(FEW_WAVES * 64) void k_linea
 template <int BYTES> __device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t offset, uint32_t to)
 {
     static_assert(BYTES == 16 || BYTES == 4, "");
-    if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+    if constexpr (BYTES == 16) asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(to), "v"(offset), "s"(base) : "memory");
+    else asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, %2" ::"{m0}"(to), "v"(offset), "s"(base) : "memory");
 }
 // All but the last N loads of every wave are there, and all waves have read what they needed.
 template <int N> __device__ __forceinline__ void arrived()
@@ -365,7 +365,7 @@ template <int N> __device__ __forceinline__ void brought()
 }
 __device__ __forceinline__ void lane_to_lds(const void* from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" ::"{m0}"(to), "v"(from) : "memory");
 }
 template <typename YT, int TM, int RING> __global__ __launch_bounds__(SPLIT_WAVES * 64, 2) void k_linear8_split(Linear8Args p)
 {
