@@ -349,14 +349,11 @@ __global__ __launch_bounds__(64 * WN * WM, WN * WM / 4) void k_linear8_many(Line
     many.run();
 }
 
-// In between: 32 channels and 32 * TM rows a workgroup, whose waves take steps of 64 columns in turn, each through a ring in LDS of its own (no
+// In between: 32 channels and 32 rows a workgroup, whose waves take steps of 64 columns in turn, each through a ring in LDS of its own (no
 // barrier until their sums meet).  A wave's i-th step has its scales in word i.
-constexpr int SPLIT_WAVES = 8;
-template <typename YT, int TM, int RING> struct Split {
-    static constexpr bool EXACT = sizeof(YT) == 4;
-    static constexpr int SLOT = (1 + TM) * 2048 + 256 * ((TM + 2) / 2), LOADS = 2 + 2 * TM + (TM + 2) / 2, LDS = SPLIT_WAVES * RING * SLOT;
-    static_assert(LDS >= SPLIT_WAVES * TM * 4096 && LDS <= 160 * 1024, "the sums meet in the rings");
-};
+constexpr int SPLIT_WAVES = 8, SPLIT_RING = 2;
+constexpr int SPLIT_SLOT = 2 * 2048 + 256, SPLIT_LOADS = 2 + 2 + 1, SPLIT_LDS = SPLIT_WAVES * SPLIT_RING * SPLIT_SLOT;      // weights, rows of x, the scales of both
+static_assert(SPLIT_LDS >= SPLIT_WAVES * 4096 && SPLIT_LDS <= 160 * 1024, "the sums meet in the rings");
 // All but the last N loads of this wave are there.
 template <int N> __device__ __forceinline__ void brought()
 {
@@ -367,93 +364,72 @@ __device__ __forceinline__ void lane_to_lds(const void* from, uint32_t to)
 {
     asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" ::"{m0}"(to), "v"(from) : "memory");
 }
-template <typename YT, int TM, int RING> __global__ __launch_bounds__(SPLIT_WAVES * 64, 2) void k_linear8_split(Linear8Args p)
+template <typename YT> __global__ __launch_bounds__(SPLIT_WAVES * 64, 2) void k_linear8_split(Linear8Args p)
 {
-    using S = Split<YT, TM, RING>;
+    constexpr bool EXACT = sizeof(YT) == 4;
     extern __shared__ __align__(16) uint8_t lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
-    const int units = channel_units(p.out_dim), unit = blockIdx.x % units, row0 = blockIdx.x / units * 32 * TM;
+    const int units = channel_units(p.out_dim), unit = blockIdx.x % units, row0 = blockIdx.x / units * 32;
     const int words = (p.blocks + 3) / 4, steps = 2 * p.blocks;
     const uint32_t width = p.blocks * E8_BLOCK;
     const uint8_t* w_at = reinterpret_cast<const uint8_t*>(p.w) + (size_t)unit * p.blocks * 4096;
     const uint8_t* x_at = p.x8 + (size_t)row0 * width;
-    uint32_t x_off[2 * TM];
+    uint32_t x_off[2];
 #pragma unroll
-    for (int c = 0; c < 2 * TM; ++c) x_off[c] = (uint32_t)min(c * 16 + (lane >> 2), p.rows - 1 - row0) * width + 16 * ((lane ^ (lane >> 4)) & 3);
-    // the scales: 32 channels' and 32 * TM rows', 64 a load
-    const uint8_t* s_at[(TM + 2) / 2];
-    int s_step[(TM + 2) / 2];
-#pragma unroll
-    for (int i = 0; i < (TM + 2) / 2; ++i) {
-        const int r = i * 64 + lane - 32;
-        s_at[i] = r < 0 ? reinterpret_cast<const uint8_t*>(p.sw + (size_t)unit * words * 32 + lane) : p.sx + (size_t)min(row0 + r, p.rows - 1) * words * 4;
-        s_step[i] = r < 0 ? 128 : 4;
-    }
-    uint8_t* ring = lds + wave * RING * S::SLOT;
+    for (int c = 0; c < 2; ++c) x_off[c] = (uint32_t)min(c * 16 + (lane >> 2), p.rows - 1 - row0) * width + 16 * ((lane ^ (lane >> 4)) & 3);
+    // the scales: 32 channels' and 32 rows', one load
+    const uint8_t* s_at = lane < 32 ? reinterpret_cast<const uint8_t*>(p.sw + (size_t)unit * words * 32 + lane) : p.sx + (size_t)min(row0 + lane - 32, p.rows - 1) * words * 4;
+    const int s_step = lane < 32 ? 128 : 4;
+    uint8_t* ring = lds + wave * SPLIT_RING * SPLIT_SLOT;
     const uint32_t ring_at = lds_address(ring);
     const int turns = steps > wave ? (steps - wave + SPLIT_WAVES - 1) / SPLIT_WAVES : 0;
     auto bring = [&](int turn) {
-        const uint32_t to = ring_at + turn % RING * S::SLOT;
+        const uint32_t to = ring_at + turn % SPLIT_RING * SPLIT_SLOT;
         const size_t step = (size_t)turn * SPLIT_WAVES + wave;
         to_lds<16>(w_at + step * 2048, lane * 16, to);
         to_lds<16>(w_at + step * 2048 + 1024, lane * 16, to + 1024);
 #pragma unroll
-        for (int c = 0; c < 2 * TM; ++c) to_lds<16>(x_at + step * 64, x_off[c], to + 2048 + c * 1024);
-#pragma unroll
-        for (int i = 0; i < (TM + 2) / 2; ++i) lane_to_lds(s_at[i] + turn * s_step[i], to + (1 + TM) * 2048 + i * 256);
+        for (int c = 0; c < 2; ++c) to_lds<16>(x_at + step * 64, x_off[c], to + 2048 + c * 1024);
+        lane_to_lds(s_at + turn * s_step, to + 4096);
     };
-    floatx16 acc[TM] = {};
-    for (int i = 0; i < RING && i < turns; ++i) bring(i);
+    floatx16 acc[1] = {};
+    for (int i = 0; i < SPLIT_RING && i < turns; ++i) bring(i);
     for (int turn = 0; turn < turns; ++turn) {
-        if (turn + RING <= turns) brought<(RING - 1) * S::LOADS>();
+        if (turn + SPLIT_RING <= turns) brought<(SPLIT_RING - 1) * SPLIT_LOADS>();
         else brought<0>();
-        const uint8_t* slot = ring + turn % RING * S::SLOT;
+        const uint8_t* slot = ring + turn % SPLIT_RING * SPLIT_SLOT;
         const uint4* w = reinterpret_cast<const uint4*>(slot) + lane;
         const uint4* x = reinterpret_cast<const uint4*>(slot + 2048) + 4 * (lane & 31);
-        const uint32_t* s = reinterpret_cast<const uint32_t*>(slot + (1 + TM) * 2048) + (lane & 31);
+        const uint32_t* s = reinterpret_cast<const uint32_t*>(slot + 4096) + (lane & 31);
         const int q = 2 * (lane >> 5) ^ (lane >> 2 & 3), shift = 8 * (wave >> 1 & 3);
-        const Frag8 wf = {w[0], w[64]};
-        const uint32_t ws = s[0];
-        Frag8 xf[TM];
-        uint32_t xs[TM];
-#pragma unroll
-        for (int m = 0; m < TM; ++m) {
-            xf[m] = Frag8{x[128 * m + q], x[128 * m + (q ^ 1)]};
-            xs[m] = s[32 + 32 * m];
-        }
+        const Frag8 wf = {w[0], w[64]}, xf = {x[q], x[q ^ 1]};
+        const uint32_t ws = s[0], xs = s[32];
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the slot is free)
-        if (turn + RING < turns) bring(turn + RING);
-        const Operand<S::EXACT> a(wf, ws >> shift & 255);
-#pragma unroll
-        for (int m = 0; m < TM; ++m) acc[m] = product(a, Operand<S::EXACT>(xf[m], xs[m] >> shift & 255), acc[m]);
+        if (turn + SPLIT_RING < turns) bring(turn + SPLIT_RING);
+        acc[0] = product(Operand<EXACT>(wf, ws >> shift & 255), Operand<EXACT>(xf, xs >> shift & 255), acc[0]);
     }
     settle(acc);
     __syncthreads();                                              // (the rings are read)
     float* sums = reinterpret_cast<float*>(lds);
 #pragma unroll
-    for (int m = 0; m < TM; ++m)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sums[((wave * TM + m) * 16 + i) * 64 + lane] = acc[m][i];
+    for (int i = 0; i < 16; ++i) sums[(wave * 16 + i) * 64 + lane] = acc[0][i];
     __syncthreads();
-    for (int job = wave; job < 4 * TM; job += SPLIT_WAVES) {
-        const int m = job >> 2, i0 = 4 * (job & 3);
-        const int n0 = unit / 2 * 64 + 32 * (lane >> 5) + 16 * (unit & 1) + i0;
-        floatx4 y = n0 < p.out_dim ? *reinterpret_cast<const floatx4*>(p.bias + n0) : floatx4{0.f, 0.f, 0.f, 0.f};
+    if (wave >= 4) return;
+    const int i0 = 4 * wave, n0 = unit / 2 * 64 + 32 * (lane >> 5) + 16 * (unit & 1) + i0;
+    floatx4 y = n0 < p.out_dim ? *reinterpret_cast<const floatx4*>(p.bias + n0) : floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < SPLIT_WAVES; ++w)
+    for (int w = 0; w < SPLIT_WAVES; ++w)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] += sums[((w * TM + m) * 16 + i0 + i) * 64 + lane];
-        store_four<YT>(p, row0 + 32 * m + (lane & 31), n0, y);
-    }
+        for (int i = 0; i < 4; ++i) y[i] += sums[(w * 16 + i0 + i) * 64 + lane];
+    store_four<YT>(p, row0 + (lane & 31), n0, y);
 }
-template <typename YT, int TM, int RING> hipError_t allow_split()
+template <typename YT> hipError_t allow_split()
 {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(k_linear8_split<YT, TM, RING>), hipFuncAttributeMaxDynamicSharedMemorySize, Split<YT, TM, RING>::LDS);
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(k_linear8_split<YT>), hipFuncAttributeMaxDynamicSharedMemorySize, SPLIT_LDS);
 }
-template <typename YT, int TM, int RING> hipError_t go_split(const Linear8Args& a, hipStream_t s)
+template <typename YT> hipError_t go_split(const Linear8Args& a, hipStream_t s)
 {
-    constexpr int LDS = Split<YT, TM, RING>::LDS;
-    hipLaunchKernelGGL((k_linear8_split<YT, TM, RING>), dim3(channel_units(a.out_dim) * ((a.rows + 32 * TM - 1) / (32 * TM))), dim3(SPLIT_WAVES * 64), LDS, s, a);
+    hipLaunchKernelGGL((k_linear8_split<YT>), dim3(channel_units(a.out_dim) * ((a.rows + 31) / 32)), dim3(SPLIT_WAVES * 64), SPLIT_LDS, s, a);
     return hipGetLastError();
 }
 
@@ -477,7 +453,7 @@ template <typename YT> hipError_t go(const Linear8Args& a, int n_cu, hipStream_t
     case Linear8Form::FEW:
         hipLaunchKernelGGL((k_linear8_few<YT>), dim3(2 * channel_units(a.out_dim)), dim3(FEW_WAVES * 64), 0, s, a);
         return hipGetLastError();
-    case Linear8Form::SPLIT: return go_split<YT, 1, 2>(a, s);
+    case Linear8Form::SPLIT: return go_split<YT>(a, s);
     case Linear8Form::TILE_64_64: return go_many<YT, 1, 1, 2, 2, 2, TWO ? 3 : 2>(a, s);
     case Linear8Form::TILE_64_128: return go_many<YT, 1, 2, 2, 2, 2, 2>(a, s);
     case Linear8Form::TILE_128_128: return go_many<YT, 2, 2, 2, 2, 2, 2>(a, s);
@@ -491,7 +467,7 @@ template <typename YT> hipError_t go(const Linear8Args& a, int n_cu, hipStream_t
 // (more than 64 KB of LDS a workgroup has to be allowed, on each device)
 template <typename YT> static hipError_t allow_all()
 {
-    hipError_t e = allow_split<YT, 1, 2>();
+    hipError_t e = allow_split<YT>();
     if (e == hipSuccess) e = allow<YT, 4, 2, 2, 2, 1, 3>();
     if (e == hipSuccess) e = allow<YT, 2, 2, 2, 2, 2, 2>();
     if (e == hipSuccess) e = allow<YT, 1, 2, 2, 2, 2, 2>();
