@@ -795,6 +795,7 @@ class Encoder:
 
 SCALE_BLOCK = 128         # columns of an 8-bit row under one scale
 NORM_RMS, NORM_NONE = 0, 1
+MAX_ROWS = 1 << 24        # of one call
 
 
 def width8(dim: int) -> int:
@@ -892,8 +893,8 @@ class Norm(_Operator):
         x_type, res_type, y_type = self._types
         count = x.numel()
         rows, rest = divmod(count, self._dim)
-        if rest:
-            raise ValueError(f"x: {tuple(x.shape)} where rows of {self._dim} are wanted")
+        if rest or rows > MAX_ROWS:
+            raise ValueError(f"x: {tuple(x.shape)} where rows of {self._dim}, {MAX_ROWS} at most, are wanted")
         a = TtsNormRows()
         a.rows = rows
         a.x, a.x_stride = self._rows(x, "x", x_type, count, rows)
@@ -955,10 +956,18 @@ class CrossBatch:
         n = len(q_len)
         if len(mem_row) != n or len(mem_len) != n:
             raise ValueError("q_len, mem_row and mem_len have a value for each request")
-        self._keep = ((C.c_int * n)(*map(int, q_len)), (C.c_longlong * n)(*map(int, mem_row)), (C.c_int * n)(*map(int, mem_len)))
+        self._keep = tuple(self._array(t, name, v) for t, name, v in ((C.c_int, "q_len", q_len), (C.c_longlong, "mem_row", mem_row), (C.c_int, "mem_len", mem_len)))
         self.queries = sum(self._keep[0])
         self.memory_rows = max((r + m for r, m in zip(self._keep[1], self._keep[2]) if m > 0), default=0)      # that k and v have to have
         self.c = TtsCrossBatch(n, *self._keep)
+
+    @staticmethod
+    def _array(ctype, name, values):
+        values = [int(v) for v in values]
+        a = (ctype * len(values))(*values)
+        if list(a) != values:                 # (ctypes takes a number's low bits)
+            raise ValueError(f"{name}: a number that {8 * C.sizeof(ctype)} bits do not hold")
+        return a
 
 
 class CrossAttention(_Operator):

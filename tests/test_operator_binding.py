@@ -1,0 +1,42 @@
+"""What the operators' Python layer refuses or hands on, without a GPU: numbers that the C types do not hold."""
+import pytest
+
+from paper_2211_13939_amd import binding
+
+
+def _bare(cls, **attributes):
+    """An object without a library behind it: tensors of the meta device pass for its device's."""
+    import torch
+    o = cls.__new__(cls)
+    o._torch, o._index, o.device, o._handle, o.calls = torch, -1, torch.device("meta"), None, []
+    o._run = lambda *a: o.calls.append(a) or 0
+    for k, v in attributes.items():
+        setattr(o, k, v)
+    return o
+
+
+@pytest.mark.parametrize("field", range(3))
+@pytest.mark.parametrize("number", [(1 << 64) + 1, -(1 << 64), 1 << 63])
+def test_lengths_that_their_types_do_not_hold(field, number):
+    lengths = [[1, 1], [0, 3], [2, 2]]
+    assert binding.CrossBatch(*lengths).queries == 2
+    lengths[field][1] = number
+    with pytest.raises(ValueError):
+        binding.CrossBatch(*lengths)
+    if field != 1:
+        lengths[field][1] = (1 << 32) + 2
+        with pytest.raises(ValueError):
+            binding.CrossBatch(*lengths)
+
+
+def test_more_rows_than_an_int_holds():
+    import torch
+    op = _bare(binding.Norm, _dim=1, _types=[torch.bfloat16] * 3)
+    y = torch.empty(5, 1, dtype=torch.bfloat16, device="meta")
+    op.run_device(y, y=y)
+    assert op.calls[0][1].rows == 5
+    for rows in ((1 << 32) + 5, 1 << 32, (1 << 24) + 1):
+        x = torch.empty(rows, 1, dtype=torch.bfloat16, device="meta")
+        with pytest.raises(ValueError):
+            op.run_device(x, y=x)
+    assert len(op.calls) == 1
