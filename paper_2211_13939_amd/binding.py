@@ -986,16 +986,19 @@ class CrossAttention(_Operator):
         return CrossBatch(q_len, mem_row, mem_len)
 
     def run_device(self, batch: CrossBatch, q, k, v, out, keep=None, lse=None, scale: float = 0.0) -> None:
-        """q, out: CUDA [queries, n_heads, head_dim]; k, v: [memory rows, n_kv_heads, head_dim], rows any multiple of 8 elements apart; keep: uint8
-        [memory rows], 0 = hidden; lse: fp32 [queries, n_heads].  Queued on the stream; scale 0: 1 / sqrt(head_dim)."""
+        """q, out: CUDA [queries, n_heads, head_dim]; k, v: [memory rows, n_kv_heads, head_dim], rows any multiple of 8 elements apart, or None where no
+        request has a memory; keep: uint8 [memory rows], 0 = hidden; lse: fp32 [queries, n_heads].  Queued on the stream; scale 0: 1 / sqrt(head_dim)."""
         t, (heads, of_q, of_k) = self._dtype, self._widths
-        queries, rows = batch.queries, k.numel() // of_k
+        if (k is None) != (v is None):
+            raise ValueError("k and v come together")
+        queries, rows = batch.queries, 0 if k is None else k.numel() // of_k
         if rows < batch.memory_rows:
             raise ValueError(f"k has {rows} rows, the batch's memories end at {batch.memory_rows}")
         a = TtsCrossTensors()
         a.q, a.q_stride = self._rows(q, "q", t, queries * of_q, queries)
-        a.k, a.k_stride = self._rows(k, "k", t, rows * of_k, rows)
-        a.v, a.v_stride = self._rows(v, "v", t, rows * of_k, rows)
+        if k is not None:
+            a.k, a.k_stride = self._rows(k, "k", t, rows * of_k, rows)
+            a.v, a.v_stride = self._rows(v, "v", t, rows * of_k, rows)
         a.out, a.out_stride = self._rows(out, "out", t, queries * of_q, queries)
         if keep is not None:
             a.keep = self._at(keep, "keep", self._torch.uint8, rows)

@@ -40,3 +40,20 @@ def test_more_rows_than_an_int_holds():
         with pytest.raises(ValueError):
             op.run_device(x, y=x)
     assert len(op.calls) == 1
+
+
+def test_no_memory_at_all():
+    """k and v are not needed where no request has any, and not to be left out otherwise or one without the other."""
+    import torch
+    op = _bare(binding.CrossAttention, _dtype=torch.float32, _widths=(2, 128, 64))
+    q, kv = (torch.empty(3, h, 64, device="meta") for h in (2, 1))
+    op.run_device(binding.CrossBatch([1, 2], [0, 5], [0, 0]), q, None, None, q)
+    t = op.calls[0][2]
+    assert t.k is None and t.v is None and t.k_stride == t.v_stride == 0
+    op.run_device(binding.CrossBatch([1, 2], [0, 1], [1, 2]), q, kv, kv, q)
+    for k, v in ((None, None), (None, kv), (kv, None)):
+        with pytest.raises(ValueError):
+            op.run_device(binding.CrossBatch([1, 2], [0, 1], [1, 2]), q, k, v, q)
+    with pytest.raises(ValueError):
+        op.run_device(binding.CrossBatch([1, 2], [0, 0], [0, 0]), q, None, kv, q)
+    assert len(op.calls) == 2
