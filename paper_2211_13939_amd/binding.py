@@ -824,6 +824,8 @@ class _Operator:
             raise ValueError(f"{device}: a GPU is wanted")
         self._index = torch.cuda.current_device() if d.index is None else d.index
         self.device = torch.device("cuda", self._index)
+        if stream is not None and stream.device != self.device:
+            raise ValueError(f"a stream of {stream.device} for an object on {self.device}")
         nbytes = int(getattr(lib(), f"tts_{self._name}_workspace_bytes")(C.byref(cfg)))
         if nbytes == 0:
             raise TtsError(TTS_E_INVAL, lib().tts_last_error().decode("utf-8", "replace"))

@@ -57,3 +57,15 @@ def test_no_memory_at_all():
     with pytest.raises(ValueError):
         op.run_device(binding.CrossBatch([1, 2], [0, 0], [0, 0]), q, None, kv, q)
     assert len(op.calls) == 2
+
+
+@pytest.mark.parametrize("make", [lambda **k: binding.Norm(binding.make_norm_config(64), [1.0] * 64, **k), lambda **k: binding.Linear8(binding.make_linear8_config(64, 32), [[1.0] * 64] * 32, **k),
+                                  lambda **k: binding.CrossAttention(binding.make_cross_config(2, 1, 64), **k)])
+def test_a_stream_of_another_device(make, monkeypatch):
+    """An object's stream takes launches of its own device: one of another is refused before anything is laid down."""
+    import torch
+    from types import SimpleNamespace
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: pytest.fail("an arena was asked for"))
+    with pytest.raises(ValueError, match="cuda:1"):
+        make(stream=SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=16), device="cuda:0")
