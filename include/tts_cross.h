@@ -62,7 +62,7 @@ typedef struct {
     void *out;      long long out_stride;
     const unsigned char *keep;    /* a byte for each memory row (of all of them, indexed as k), 0 = hidden; null: none is */
     float *lse;                   /* fp32 [queries][n_heads], 4-byte aligned; null: not wanted */
-    float scale;                  /* > 0, finite; 0: 1 / sqrt(head_dim) */
+    float scale;                  /* > 0, at most 2^127; 0: 1 / sqrt(head_dim) */
 } tts_cross_tensors;
 
 /* Bytes of device memory tts_cross_create needs for this configuration (0 if the configuration is invalid). */
@@ -78,7 +78,7 @@ int tts_cross_create(const tts_cross_config *cfg, void *dev_arena, size_t arena_
  * Attend, asynchronously on the stream (the batch's arrays are consumed before the call returns).
  * Errors: TTS_E_INVAL for null pointers, a number of requests, a length or a row outside its range, more than 2^31 - 1 queries or 2^23 tiles in all
  * (a tile: 16 pairs of a query and a head, of one request and one head of k),
- * a stride that is too small, too large or no multiple of 8, an array that is not aligned, or a scale that is negative or not finite.
+ * a stride that is too small, too large or no multiple of 8, an array that is not aligned, or a scale that is negative or, times log2(e), not finite.
  */
 int tts_cross_run(tts_cross *att, const tts_cross_batch *batch, const tts_cross_tensors *tensors);
 

@@ -1007,6 +1007,8 @@ class CrossAttention(_Operator):
         if lse is not None:
             a.lse = self._at(lse, "lse", self._torch.float32, queries * heads)
         a.scale = scale
+        if scale and not a.scale:
+            raise ValueError(f"a scale of {scale} is 0 in fp32")
         rc = self._run(self._handle, batch.c, a)
         if rc:
             _check(rc)

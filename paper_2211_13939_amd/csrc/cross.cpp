@@ -90,7 +90,8 @@ extern "C" int tts_cross_run(tts_cross* p, const tts_cross_batch* b, const tts_c
         memory += b->mem_len[i];
     }
     if (queries > 0x7FFFFFFF) return fail(TTS_E_INVAL, "%lld queries in one call", queries);
-    if (!(t->scale >= 0 && std::isfinite(t->scale))) return fail(TTS_E_INVAL, "scale must be finite and not negative");
+    const float scale = (t->scale > 0 ? t->scale : 1.0f / sqrtf((float)p->cfg.head_dim)) * 1.4426950408889634f;       // times log2(e)
+    if (!(t->scale >= 0 && std::isfinite(scale))) return fail(TTS_E_INVAL, "scale must not be negative, and finite times log2(e)");
     if (queries == 0) return TTS_OK;
     if (!t->q || !t->out || (memory && (!t->k || !t->v))) return fail(TTS_E_INVAL, "null argument");
     struct { const char* name; const void* at; long long stride; int heads; } arrays[4] = {{"q", t->q, t->q_stride, p->cfg.n_heads}, {"k", t->k, t->k_stride, p->cfg.n_kv_heads},
@@ -110,7 +111,7 @@ extern "C" int tts_cross_run(tts_cross* p, const tts_cross_batch* b, const tts_c
     a.parts = p->parts;
     a.zeros = p->zeros;
     a.q_stride = stride[0]; a.k_stride = stride[1]; a.v_stride = stride[2]; a.out_stride = stride[3];
-    a.scale = (t->scale > 0 ? t->scale : 1.0f / sqrtf((float)p->cfg.head_dim)) * 1.4426950408889634f;
+    a.scale = scale;
     a.n_heads = p->cfg.n_heads; a.n_kv_heads = p->cfg.n_kv_heads; a.head_dim = p->cfg.head_dim;
     OnDevice on(p->device);
     HIP_TRY(on.err);

@@ -1,7 +1,10 @@
-"""What the operators' Python layer refuses or hands on, without a GPU: numbers that the C types do not hold."""
+"""What the operators' Python layer refuses or hands on, and their host code's last refusals, without a GPU: numbers that the C types do not hold."""
+import ctypes as C
+
 import pytest
 
 from paper_2211_13939_amd import binding
+from tests.test_operators_host import INVAL, Made, lib  # noqa: F401  (a fixture)
 
 
 def _bare(cls, **attributes):
@@ -69,3 +72,22 @@ def test_a_stream_of_another_device(make, monkeypatch):
     monkeypatch.setattr(torch, "empty", lambda *a, **k: pytest.fail("an arena was asked for"))
     with pytest.raises(ValueError, match="cuda:1"):
         make(stream=SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=16), device="cuda:0")
+
+
+def test_scales_at_the_ends_of_fp32(lib):      # noqa: F811
+    """Kernels take the scale times log2(e), which has to be a number too; one that fp32 rounds to 0 would be the default in the place of next to nothing."""
+    import torch
+    lib.fake_reset()
+    m = Made(lib, "cross", binding.make_cross_config(2, 1, 64))
+    b = binding.CrossBatch([1], [0], [1])
+    for scale, rc in ((2.0 ** 127, 0), (2.3e38, 0), (2.4e38, INVAL), (3.4e38, INVAL), (1e-44, 0)):
+        t = binding.TtsCrossTensors(q=1 << 20, k=2 << 20, v=3 << 20, out=4 << 20, scale=scale)
+        assert lib.tts_cross_run(m.h, C.byref(b.c), C.byref(t)) == rc, scale
+    m.close()
+    op = _bare(binding.CrossAttention, _dtype=torch.float32, _widths=(2, 128, 64))
+    q, kv = (torch.empty(1, h, 64, device="meta") for h in (2, 1))
+    op.run_device(b, q, kv, kv, q, scale=1e-44)
+    op.run_device(b, q, kv, kv, q)
+    assert op.calls[0][2].scale > 0 and op.calls[1][2].scale == 0
+    with pytest.raises(ValueError):
+        op.run_device(b, q, kv, kv, q, scale=1e-46)
