@@ -11,7 +11,9 @@
  * and behind a request's memory is not used, whatever it is (infinities and NaN included).
  *
  * Sums, the softmax's maximum and sum and the outputs' sums are fp32; bf16 weights w are rounded to bf16 for their
- * product with v (relative error up to 2^-8 each).  One call = one dynamic batch of requests of any lengths, from one query (a
+ * product with v (relative error up to 2^-8 each).  The order of a request's sums follows from all lengths of the call (whether its memory is read in
+ * parts, and of which length, and which kernel takes it): a call repeats itself bit for bit, but a request in other company may differ in its last bits, unlike in the
+ * pool.  One call = one dynamic batch of requests of any lengths, from one query (a
  * step) to many (all frames at once).  Everything is queued on the stream given at creation; device memory comes from the caller's
  * arena; nothing is allocated on the device.  The lengths travel with the launches: a call may be captured, and its
  * graph holds the lengths it was captured with.  Long memories that few queries attend are split, and the parts

@@ -14,6 +14,9 @@
  * a scale from 2^-124 to 2^119 exactly.  In blocks whose largest magnitude is at most 448 * 2^-125, of either operand, it rounds operands to multiples
  * of 2^-133; in those where it is above 448 * 2^119 (2.98e38) numbers of 256 * 2^120 and more become infinite.  bf16 results know no such limits.
  *
+ * The order of a row's sums is fixed for a number of rows, in_dim and out_dim, and another for some other numbers of rows (the kernel's tiles follow from
+ * them): a call repeats itself bit for bit, but a row in a call of more or fewer rows may differ in its last bits, unlike in the pool, whose requests do not depend on each other.
+ *
  * Everything is queued on the stream given at creation; device memory comes from the caller's arena; nothing is
  * allocated on the device.  A call is one launch and may be captured into a graph.
  * Conventions as in tts_pool.h: 0 on success, negative tts_status otherwise, text in tts_last_error(); one owner

@@ -16,8 +16,9 @@
  * y8 rows are TTS_WIDTH8(dim) bytes: columns past dim are zeros.  scales rows are TTS_SCALE_COLUMNS(dim) bytes: what lies
  * past the last block is 127.
  *
- * Sums are fp32, formed in an order that depends on dim and rows alone; of a row whose squares leave fp32's range they are those of the row
- * times a power of two, so that rows of any finite magnitude have their norm.  (A row of zeros without an eps is NaN, as is one with a NaN.)  Everything is queued on the stream given
+ * Sums are fp32, formed in an order that depends on dim and the number of rows alone (calls of many rows have another: a row may differ
+ * there in its last bits).  Of a row whose squares leave fp32's range they are those of the row times a power of two, so that rows of any finite
+ * magnitude have their norm; a row of zeros without an eps is NaN, as is one with a NaN.  Everything is queued on the stream given
  * at creation; device memory comes from the caller's arena; nothing is allocated on the device.  A call is one
  * launch and may be captured into a graph.  Conventions as in tts_pool.h: 0 on success, negative tts_status otherwise,
  * text in tts_last_error(); one owner thread per object.

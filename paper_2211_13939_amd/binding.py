@@ -809,7 +809,8 @@ def scale_columns(dim: int) -> int:
 
 
 class _Operator:
-    """An object on a stream with an arena of its own, as the modules above have them."""
+    """An object on a stream with an arena of its own, as the modules above have them.  Calls are queued on that stream (None: a new one) whichever is current, and wait for no other: what a call
+    reads has to be there in that stream's order, and its tensors are the caller's to keep until the stream has come this far."""
 
     _name = ""
 
@@ -891,7 +892,7 @@ class Norm(_Operator):
 
     def run_device(self, x, res=None, total=None, y=None, y8=None, scales=None) -> None:
         """x, res, total, y: CUDA [rows, dim] of the configuration's types, rows any distance apart; y8: float8_e4m3fn [rows, width8(dim)],
-        scales: float8_e8m0fnu [rows, scale_columns(dim)].  Those that are None are not there.  Queued on the stream."""
+        scales: float8_e8m0fnu [rows, scale_columns(dim)].  Those that are None are not there.  Queued on the object's stream."""
         x_type, res_type, y_type = self._types
         count = x.numel()
         rows, rest = divmod(count, self._dim)
@@ -936,7 +937,7 @@ class Linear8(_Operator):
 
     def run_device(self, x8, scales, y) -> None:
         """x8: CUDA float8_e4m3fn [rows, width8(in_dim)], zeros past in_dim; scales: float8_e8m0fnu [rows, scale_columns(in_dim)]; y: [rows, out_dim],
-        rows any distance apart.  Queued on the stream."""
+        rows any distance apart.  Queued on the object's stream."""
         k, n_scales, n = self._widths
         rows = x8.numel() // k
         at = self._at(x8, "x8", self._types8[0], rows * k)
@@ -989,7 +990,7 @@ class CrossAttention(_Operator):
 
     def run_device(self, batch: CrossBatch, q, k, v, out, keep=None, lse=None, scale: float = 0.0) -> None:
         """q, out: CUDA [queries, n_heads, head_dim]; k, v: [memory rows, n_kv_heads, head_dim], rows any multiple of 8 elements apart, or None where no
-        request has a memory; keep: uint8 [memory rows], 0 = hidden; lse: fp32 [queries, n_heads].  Queued on the stream; scale 0: 1 / sqrt(head_dim)."""
+        request has a memory; keep: uint8 [memory rows], 0 = hidden; lse: fp32 [queries, n_heads].  Queued on the object's stream; scale 0: 1 / sqrt(head_dim)."""
         t, (heads, of_q, of_k) = self._dtype, self._widths
         if (k is None) != (v is None):
             raise ValueError("k and v come together")

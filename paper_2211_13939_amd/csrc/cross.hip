@@ -112,6 +112,8 @@ template <typename T, int D, bool FULL, bool MASK> struct Keys {
     __device__ __forceinline__ void add(const float* w, floatx4* o) const
     {
         if constexpr (sizeof(T) == 2) {
+            // (weights to bf16, the values' type: each off by up to 2^-8 of itself, so that the result is by no more than that before its own rounding, which is as large; two
+            // products, of their upper and lower halves, would keep them at twice the matrix instructions)
             const uint4 b = make_uint4(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7]));
 #pragma unroll
             for (int e = 0; e < G::NE; ++e) {
@@ -531,7 +533,7 @@ template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW,
         const int turn = D == 128 ? lane >> 2 & 3 : lane >> 3 & 1;
 #pragma unroll
         for (int k = 0; k < 2 * N; ++k) {
-            uint4 w;
+            uint4 w;                                     // (rounded to bf16, as in Keys::add)
             const int i = 8 * (k & 1);
             w.x = pack_bf16x2(s[k / 2][i], s[k / 2][i + 1]);
             w.y = pack_bf16x2(s[k / 2][i + 2], s[k / 2][i + 3]);
