@@ -395,7 +395,8 @@ template <int N> __device__ __forceinline__ void arrived()
 // (written out as in linear8.hip: no registers to come back to)
 __device__ __forceinline__ void to_lds(const char* from, uint32_t to)
 {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(to), "v"(from) : "memory");
+    uint32_t m0;
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off" : "={m0}"(m0) : "s"(to), "v"(from) : "memory");
 }
 
 // (128 registers where heads are narrow and tiles large: with 135 of them 3 waves in place of 4 share a SIMD, and 16 heads of 3000 x 3000 x 64 in eight requests

@@ -135,12 +135,14 @@ template <typename YT> __global__ __launch_bounds__(FEW_WAVES * 64) void k_linea
 // operand's reads of 16 bytes find all banks.
 //
 // These loads are written out: of the builtin the compiler does not know which of two buffers it fills, and waits for it in front of every read of the
-// other.  They have no registers to come back to; what they bring is there behind arrived().
+// other.  They have no registers to come back to; what they bring is there behind arrived().  m0, where it goes, is
+// theirs: they set it themselves, and its old value is no longer there.
 template <int BYTES> __device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t offset, uint32_t to)
 {
     static_assert(BYTES == 16 || BYTES == 4, "");
-    if constexpr (BYTES == 16) asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(to), "v"(offset), "s"(base) : "memory");
-    else asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, %2" ::"{m0}"(to), "v"(offset), "s"(base) : "memory");
+    uint32_t m0;
+    if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" : "={m0}"(m0) : "s"(to), "v"(offset), "s"(base) : "memory");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, %3" : "={m0}"(m0) : "s"(to), "v"(offset), "s"(base) : "memory");
 }
 // All but the last N loads of every wave are there, and all waves have read what they needed.
 template <int N> __device__ __forceinline__ void arrived()
@@ -362,7 +364,8 @@ template <int N> __device__ __forceinline__ void brought()
 }
 __device__ __forceinline__ void lane_to_lds(const void* from, uint32_t to)
 {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" ::"{m0}"(to), "v"(from) : "memory");
+    uint32_t m0;
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, off" : "={m0}"(m0) : "s"(to), "v"(from) : "memory");
 }
 template <typename YT> __global__ __launch_bounds__(SPLIT_WAVES * 64, 2) void k_linear8_split(Linear8Args p)
 {
