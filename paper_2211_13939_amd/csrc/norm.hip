@@ -4,7 +4,7 @@
 // Bound by bytes (some 6 operations an element).  A lane holds chunks of 8 neighbouring columns, so that loads and stores are 16 or 32
 // bytes a lane and 16 lanes hold a block of 128: its largest magnitude is found by four exchanges inside a row of 16 lanes.  Rows of up to
 // 2048 columns are a wave's in large calls (no barrier); wider ones, and those of calls with fewer rows than the chip has waves for, a
-// workgroup's.  us: 16384 x 4096 with residual, total and 8-bit rows 82 (468 MB, 5.7 TB/s), 8574 x 896 fp32 to fp32 and 8 bits 16 (69 MB), one row of 512 2.2 in a graph.
+// workgroup's.  us: 16384 x 4096 with residual, total and 8-bit rows 82 (468 MB, 5.7 TB/s), 8574 x 896 fp32 to fp32 and 8 bits 16 (69 MB), one row of 512 2.3 in a graph.
 #include "operator_kernels.h"
 #include "mfma.h"
 
