@@ -52,6 +52,9 @@ EXPORTS = (
 # every symbol include/tts_norm.h, tts_linear8.h and tts_cross.h declare
 OPERATOR_EXPORTS = tuple(f"tts_{op}_{call}" for op in ("norm", "linear8", "cross") for call in ("workspace_bytes", "create", "run", "destroy"))
 
+# every symbol include/tts_rotary.h and tts_cache.h declare
+PAST_EXPORTS = tuple(f"tts_{op}_{call}" for op in ("rotary", "cache") for call in ("workspace_bytes", "create", "run", "destroy"))
+
 _fp = C.POINTER(C.c_float)
 _ip = C.POINTER(C.c_int)
 _i64p = C.POINTER(C.c_int64)
@@ -117,6 +120,33 @@ class TtsCrossTensors(C.Structure):
     _fields_ = [("q", C.c_void_p), ("q_stride", C.c_longlong), ("k", C.c_void_p), ("k_stride", C.c_longlong),
                 ("v", C.c_void_p), ("v_stride", C.c_longlong), ("out", C.c_void_p), ("out_stride", C.c_longlong),
                 ("keep", C.c_void_p), ("lse", C.c_void_p), ("scale", C.c_float)]
+
+
+class TtsRotaryAngles(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("rot_dim", "layout", "scaling", "trained_len")] + [(n, C.c_double) for n in ("base", "factor", "low", "high", "magnitude")]
+
+
+class TtsRotaryConfig(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("n_heads", "head_dim", "x_dtype", "y_dtype")] + [("angles", TtsRotaryAngles)]
+
+
+class TtsRotaryRows(C.Structure):
+    _fields_ = [("rows", C.c_int), ("x", C.c_void_p), ("x_stride", C.c_longlong), ("y", C.c_void_p), ("y_stride", C.c_longlong),
+                ("positions", C.c_void_p), ("first", C.c_int), ("back", C.c_int)]
+
+
+class TtsCacheConfig(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("n_kv_heads", "n_heads", "head_dim", "page_rows", "x_dtype", "dtype")] + [("angles", TtsRotaryAngles)]
+
+
+class TtsCacheBatch(C.Structure):
+    _fields_ = [("n", C.c_int), ("len", _ip), ("row", _ip), ("table_row", _ip), ("position", _ip)]
+
+
+class TtsCacheTensors(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("k_stride", C.c_longlong), ("v", C.c_void_p), ("v_stride", C.c_longlong), ("q", C.c_void_p), ("q_stride", C.c_longlong),
+                ("q_out", C.c_void_p), ("q_out_stride", C.c_longlong), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_longlong),
+                ("n_pages", C.c_int), ("table", C.c_void_p), ("table_rows", C.c_int), ("table_cols", C.c_int)]
 
 
 VOCODER_HOP = 256
@@ -225,7 +255,12 @@ def lib() -> C.CDLL:
     L.tts_cross_workspace_bytes.argtypes = [C.POINTER(TtsCrossConfig)]
     L.tts_cross_create.argtypes = [C.POINTER(TtsCrossConfig), vp, C.c_size_t, vp, C.POINTER(vp)]
     L.tts_cross_run.argtypes = [vp, C.POINTER(TtsCrossBatch), C.POINTER(TtsCrossTensors)]
-    for f in (L.tts_norm_destroy, L.tts_linear8_destroy, L.tts_cross_destroy):
+    for op, config, *args in (("rotary", TtsRotaryConfig, C.POINTER(TtsRotaryRows)), ("cache", TtsCacheConfig, C.POINTER(TtsCacheBatch), C.POINTER(TtsCacheTensors))):
+        f = getattr(L, f"tts_{op}_workspace_bytes")
+        f.restype, f.argtypes = C.c_size_t, [C.POINTER(config)]
+        getattr(L, f"tts_{op}_create").argtypes = [C.POINTER(config), vp, C.c_size_t, vp, C.POINTER(vp)]
+        getattr(L, f"tts_{op}_run").argtypes = [vp, *args]
+    for f in (L.tts_norm_destroy, L.tts_linear8_destroy, L.tts_cross_destroy, L.tts_rotary_destroy, L.tts_cache_destroy):
         f.restype = None
         f.argtypes = [vp]
     _lib = L
@@ -1010,6 +1045,127 @@ class CrossAttention(_Operator):
         a.scale = scale
         if scale and not a.scale:
             raise ValueError(f"a scale of {scale} is 0 in fp32")
+        rc = self._run(self._handle, batch.c, a)
+        if rc:
+            _check(rc)
+
+
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
+ROTARY_MAX_ROWS = 1 << 24  # of one call
+
+
+def make_rotary_angles(rot_dim: int, pairs: bool = False, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0, trained_len: int = 0, low: float = 1.0, high: float = 32.0,
+                       magnitude: float = 1.0) -> TtsRotaryAngles:
+    return TtsRotaryAngles(int(rot_dim), int(bool(pairs)), int(scaling), int(trained_len), float(base), float(factor), float(low), float(high), float(magnitude))
+
+
+def make_rotary_config(n_heads: int, head_dim: int, angles: TtsRotaryAngles, x_bf16: bool = False, y_bf16: bool = False) -> TtsRotaryConfig:
+    pick = lambda b: DTYPE_BF16 if b else DTYPE_F32   # noqa: E731
+    return TtsRotaryConfig(int(n_heads), int(head_dim), pick(x_bf16), pick(y_bf16), angles)
+
+
+class Rotary(_Operator):
+    """tts_rotary_* calls: heads' columns turned in pairs to their rows' positions."""
+
+    _name = "rotary"
+
+    def __init__(self, cfg: TtsRotaryConfig, stream=None, device: str = "cuda:0"):
+        where = self._setup(cfg, stream, device)
+        _check(lib().tts_rotary_create(C.byref(cfg), *where))
+        self._types = (self._type(cfg.x_dtype), self._type(cfg.y_dtype), self._torch.int32)
+        self._width = cfg.n_heads * cfg.head_dim
+
+    def run_device(self, x, y, positions=None, first: int = 0, back: bool = False) -> None:
+        """x, y: CUDA [rows, n_heads, head_dim] of the configuration's types, rows any multiple of 8 elements apart; y may be x.  positions: int32 [rows], or None: row r is at
+        first + r.  back: the other way, as the gradient is.  Queued on the object's stream."""
+        count = x.numel()
+        rows, rest = divmod(count, self._width)
+        if rest or rows > ROTARY_MAX_ROWS:
+            raise ValueError(f"x: {tuple(x.shape)} where rows of {self._width}, {ROTARY_MAX_ROWS} at most, are wanted")
+        a = TtsRotaryRows()
+        a.rows = rows
+        a.x, a.x_stride = self._rows(x, "x", self._types[0], count, rows)
+        a.y, a.y_stride = self._rows(y, "y", self._types[1], count, rows)
+        if positions is not None:
+            a.positions = self._at(positions, "positions", self._types[2], rows)
+        elif not -(1 << 31) <= first < 1 << 31:
+            raise ValueError(f"first: {first} is a number that 32 bits do not hold")
+        else:
+            a.first = first
+        a.back = bool(back)
+        rc = self._run(self._handle, a)
+        if rc:
+            _check(rc)
+
+
+def make_cache_config(n_kv_heads: int, head_dim: int, page_rows: int, angles: Optional[TtsRotaryAngles] = None, n_heads: int = 0, bf16: bool = False, x_bf16: bool = False) -> TtsCacheConfig:
+    """angles None: nothing turns; n_heads 0: no queries come along."""
+    pick = lambda b: DTYPE_BF16 if b else DTYPE_F32   # noqa: E731
+    return TtsCacheConfig(int(n_kv_heads), int(n_heads), int(head_dim), int(page_rows), pick(x_bf16), pick(bf16), angles if angles is not None else TtsRotaryAngles())
+
+
+class CacheBatch:
+    """The numbers of a dynamic batch's new rows: how many, where the first of them goes, the sequence's row of the table, the first one's position (None: where it goes)."""
+
+    def __init__(self, length, row, table_row, position=None):
+        n = len(length)
+        if len(row) != n or len(table_row) != n or (position is not None and len(position) != n):
+            raise ValueError("length, row, table_row and position have a value for each request")
+        self._keep = [None if v is None else CrossBatch._array(C.c_int, name, v) for name, v in (("length", length), ("row", row), ("table_row", table_row), ("position", position))]
+        self.rows = sum(self._keep[0])
+        self.c = TtsCacheBatch(n, *self._keep)
+
+
+class _Paged(_Operator):
+    """An operator on a paged cache."""
+
+    def _setup_pages(self, cfg):
+        self._pages_type, self._int = self._type(cfg.dtype), self._torch.int32
+        self._page = cfg.n_kv_heads * cfg.page_rows * cfg.head_dim
+
+    def _pages(self, a, k_pages, v_pages, table) -> None:
+        n, rest = divmod(k_pages.numel(), self._page)
+        if rest or n >= 1 << 31:
+            raise ValueError(f"k_pages: {tuple(k_pages.shape)} where pages of {self._page} elements are wanted")
+        a.k_pages, a.page_stride = self._rows(k_pages, "k_pages", self._pages_type, n * self._page, n)
+        a.v_pages, v_stride = self._rows(v_pages, "v_pages", self._pages_type, n * self._page, n)
+        if n > 1 and (a.page_stride or self._page) != (v_stride or self._page):
+            raise ValueError(f"pages of keys lie {a.page_stride or self._page} elements apart, those of values {v_stride or self._page}")
+        if table.dim() != 2 or table.shape[0] >= 1 << 31 or table.shape[1] >= 1 << 31:
+            raise ValueError(f"table: {tuple(table.shape)} where [sequences, pages] is wanted")
+        a.n_pages, (a.table_rows, a.table_cols) = n, table.shape
+        a.table = self._at(table, "table", self._int, table.numel())
+
+
+class Cache(_Paged):
+    """tts_cache_* calls: new rows of keys (turned to their positions) and values on their way to a paged cache, queries beside them."""
+
+    _name = "cache"
+
+    def __init__(self, cfg: TtsCacheConfig, stream=None, device: str = "cuda:0"):
+        where = self._setup(cfg, stream, device)
+        _check(lib().tts_cache_create(C.byref(cfg), *where))
+        self._setup_pages(cfg)
+        self._x_type, self._widths = self._type(cfg.x_dtype), (cfg.n_kv_heads * cfg.head_dim, cfg.n_heads * cfg.head_dim)
+
+    def batch(self, length, row, table_row, position=None) -> CacheBatch:
+        """A batch's numbers, for any number of calls."""
+        return CacheBatch(length, row, table_row, position)
+
+    def run_device(self, batch: CacheBatch, k, v, k_pages, v_pages, table, q=None, q_out=None) -> None:
+        """k, v: CUDA [new rows, n_kv_heads, head_dim], q: [new rows, n_heads, head_dim], rows any multiple of 8 elements apart; q_out: as q, of the cache's type (or q itself);
+        k_pages, v_pages: [pages, n_kv_heads, page_rows, head_dim], pages any multiple of 8 elements apart; table: int32 [sequences, pages], other numbers than 0 .. pages - 1 for
+        what is no page.  Queued on the object's stream."""
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out come together")
+        rows, (of_k, of_q) = batch.rows, self._widths
+        a = TtsCacheTensors()
+        a.k, a.k_stride = self._rows(k, "k", self._x_type, rows * of_k, rows)
+        a.v, a.v_stride = self._rows(v, "v", self._x_type, rows * of_k, rows)
+        if q is not None:
+            a.q, a.q_stride = self._rows(q, "q", self._x_type, rows * of_q, rows)
+            a.q_out, a.q_out_stride = self._rows(q_out, "q_out", self._pages_type, rows * of_q, rows)
+        self._pages(a, k_pages, v_pages, table)
         rc = self._run(self._handle, batch.c, a)
         if rc:
             _check(rc)
