@@ -1,12 +1,8 @@
 // Cross attention: every query row of a request attends the request's memory, o = softmax(scale * q k^T) v, several query heads to a head of
 // k and v.  One pass over the memory with the softmax's running maximum and sum; rows of a request and a key head are its
 // (query, head of the group) pairs, 16 to a tile, so that heads which share keys share their loads too.
-//
-// Scores are formed transposed, keys as the matrix instruction's rows: a lane then holds four neighbouring keys of ONE query row, and so
-// do its exponentials, which are the second product's operand (values as rows, query rows as columns) without leaving their registers.  The second product
-// sums over keys in whatever order both operands share.
 #include "operator_kernels.h"
-#include "mfma.h"
+#include "attend.h"
 
 #include <algorithm>
 #include <cmath>
@@ -19,30 +15,6 @@ namespace {
 constexpr int FEW_WAVES = 4;
 constexpr int MAX_PARTS = 2048, MAX_SPLITS = 256;    // parts of one launch, of one row tile
 constexpr int part_floats(int d) { return 16 * (d + 2); }
-
-// of the four lanes that share l % 16
-__device__ __forceinline__ float across_max(float x)
-{
-    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-__device__ __forceinline__ float across_sum(float x)
-{
-    x += __shfl_xor(x, 16, 64);
-    return x + __shfl_xor(x, 32, 64);
-}
-
-// A step's keys of a wave.  Lane l, group g = l / 16.  First operand: rows of keys, the lane's is key l % 16 of each 16; second: of the keys that
-// the lane holds scores of, 4 g .. 4 g + 3 of each 16, the D / 16 columns from (D / 16) * (l % 16) on.  Row i of the second product's tile
-// e is then column (D / 16) * i + e of the head.
-// FULL: heads are D wide.  Of narrower ones the first operand's missing columns are zeros; the second's are any (nobody stores what comes of them).
-template <typename T, int D> struct Geometry {
-    static constexpr int PER_LANE = sizeof(T) == 2 ? 8 : 4, N = 4 * PER_LANE, TILES = N / 16;       // scores of a lane, keys of a step
-    static constexpr int EPL = 16 / sizeof(T), NF = D / (4 * EPL), NE = D / 16;                      // elements of 16 bytes, loads of a key, columns of a lane
-    static __device__ __forceinline__ int key(int i, int g) { return 16 * (i / 4) + 4 * g + (i & 3); }      // of the lane's i-th score
-};
 
 // Where a lane's parts of a step lie, in bytes from the step's first key
 template <typename T, int D> struct Places {
@@ -60,11 +32,11 @@ template <typename T, int D> struct Places {
     }
 };
 
-template <typename T, int D, bool FULL, bool MASK> struct Keys {
+template <typename T, int D, bool FULL, bool MASK> struct Keys : Operands<T, D> {
     using G = Geometry<T, D>;
+    using Operands<T, D>::k;
+    using Operands<T, D>::v;
     uint8_t seen[G::PER_LANE];
-    uint4 k[G::TILES][G::NF];
-    uint32_t v[G::PER_LANE][G::NE * sizeof(T) / 4];
     // kp, vp, keep: the step's first key; last: the last of its keys that there is, counted from 0, k_last, v_last: where that lies (keys behind it are
     // loaded from there)
     __device__ __forceinline__ void load(const char* kp, const char* vp, const uint8_t* keep, const Places<T, D>& at, int last, uint32_t k_last, uint32_t v_last, int head_dim, int lane)
@@ -97,38 +69,6 @@ template <typename T, int D, bool FULL, bool MASK> struct Keys {
         }
         // (left alone, the compiler puts them in front of their use: 26 requests of 2185 .. 2925 keys, 8 fp32 heads of 128, 171 in place of 101 us)
         if constexpr (MASK) __builtin_amdgcn_sched_barrier(0);
-    }
-    __device__ __forceinline__ void scores(const uint4 (&q)[G::NF], float* s) const
-    {
-#pragma unroll
-        for (int t = 0; t < G::TILES; ++t) {
-            floatx4 a = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int f = 0; f < G::NF; ++f) a = mfma_frag<T>(k[t][f], q[f], a);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[4 * t + j] = a[j];
-        }
-    }
-    __device__ __forceinline__ void add(const float* w, floatx4* o) const
-    {
-        if constexpr (sizeof(T) == 2) {
-            // (weights to bf16, the values' type: each off by up to 2^-8 of itself, so that the result is by no more than that before its own rounding, which is as large; two
-            // products, of their upper and lower halves, would keep them at twice the matrix instructions)
-            const uint4 b = make_uint4(pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7]));
-#pragma unroll
-            for (int e = 0; e < G::NE; ++e) {
-                const uint32_t half = e & 1 ? 0x07060302u : 0x05040100u;     // the upper or lower halves of two words
-                uint32_t a[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(v[2 * i + 1][e / 2], v[2 * i][e / 2], half);
-                o[e] = mfma_frag<bf16_t>(make_uint4(a[0], a[1], a[2], a[3]), b, o[e]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < G::PER_LANE; ++i)
-#pragma unroll
-                for (int e = 0; e < G::NE; ++e) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i][e]), w[i], o[e], 0, 0, 0);
-        }
     }
 };
 
@@ -185,18 +125,6 @@ template <bool ROWS = false, typename Args> __device__ __forceinline__ int reque
 
 // (one without keys, too, where there are none)
 __host__ __device__ __forceinline__ int parts_of(const CrossReq& r, int share) { return r.mem_len <= share ? 1 : (r.mem_len - 1) / share + 1; }
-
-// D / 16 neighbouring columns of a row
-template <typename T, int NE> __device__ __forceinline__ void store_columns(T* at, const float* v)
-{
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int e = 0; e < NE; e += 4) *reinterpret_cast<float4*>(at + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < NE; e += 4) *reinterpret_cast<uint2*>(at + e) = make_uint2(pack_bf16x2(v[e], v[e + 1]), pack_bf16x2(v[e + 2], v[e + 3]));
-    }
-}
 
 // The rows of a tile from the parts of its memory: maximum and sum, then columns.  `m` in units of log2; at(part) gives a part's maximum, sum and columns.
 template <typename T, int D, typename At>
@@ -374,37 +302,17 @@ template <typename T, int D, typename Args> __global__ __launch_bounds__(JOIN) v
 // Many rows, two bytes: 32 * NW rows of a request and a key head, 32 a wave, over the memory in tiles of 64 keys that all waves read from LDS while
 // the next R - 1 are on their way there, 16 bytes a lane straight from memory; one barrier a tile.
 //
-// Scores are transposed as above, of 32 keys and 32 rows an instruction: lane l holds row l % 32 and of each 16 keys 4 h .. 4 h + 3 and 8 + 4 h .. + 3
-// (h = l / 32), which are eight of the second product's operand.  Its other operand, values with the keys along a lane, comes by LDS's transposing
-// reads.  Keys' 16-byte pieces and values' 64-byte ones change places from row to row, so that reads down a column find all banks.
-// Positions that are hidden or not there are loaded from zeros.  The sums are rescaled when a row's maximum has grown by more than 2^8: weights are at most
-// that large until then, and their quotient is the same.
-constexpr int KEYS = 64;
-typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef short shortx4 __attribute__((ext_vector_type(4)));
+// Positions that are hidden or not there are loaded from zeros.
 template <int D, int NW, int R> struct ManyRows {
     static constexpr int ROW = 2 * D, PART = KEYS * ROW, SLOT = 2 * PART, LOADS = PART / 1024 / NW, LDS = R * SLOT + 2 * KEYS * 8;
     static_assert(LOADS * 1024 * NW == PART, "shares of the waves");
 };
-// All but the last N loads of every wave are there, and all waves have read what they needed.
-template <int N> __device__ __forceinline__ void arrived()
-{
-    static_assert(N < 64, "the counter has six bits");
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-}
-// (written out as in linear8.hip: no registers to come back to)
-__device__ __forceinline__ void to_lds(const char* from, uint32_t to)
-{
-    uint32_t m0;
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off" : "={m0}"(m0) : "s"(to), "v"(from) : "memory");
-}
-
 // (128 registers where heads are narrow and tiles large: with 135 of them 3 waves in place of 4 share a SIMD, and 16 heads of 3000 x 3000 x 64 in eight requests
 // take 366 in place of 328 us)
 template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : NW == 8 ? 4 : 3) void k_cross_many(CrossArgs p)
 {
     using M = ManyRows<D, NW, R>;
-    constexpr int ROW = M::ROW, ND = D / 32, NK = D / 16;
+    constexpr int ROW = M::ROW, NK = D / 16;
     extern __shared__ __align__(16) char lds[];
     uint64_t* masks = reinterpret_cast<uint64_t*>(lds + R * M::SLOT);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
@@ -416,12 +324,12 @@ template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW,
     const int kv = (id - r.first) / tiles, row = ((id - r.first) % tiles * NW + wave) * 32 + c, row_there = min(row, rows - 1);
     const long long q_row = (long long)r.q_row + row_there / group;
     const int head = kv * group + row_there % group;
-    uint4 q[NK];
+    ManyRunning<D> run;
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
         const int d = 16 * k + 8 * h;
         const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(p.q) + q_row * p.q_stride + head * p.head_dim + (d < p.head_dim ? d : 0));
-        q[k] = d < p.head_dim ? x : make_uint4(0, 0, 0, 0);
+        run.q[k] = d < p.head_dim ? x : make_uint4(0, 0, 0, 0);
     }
     const int n_tiles = (r.mem_len + KEYS - 1) / KEYS;
     const long long k_row = 2 * p.k_stride, v_row = 2 * p.v_stride;
@@ -432,7 +340,7 @@ template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW,
 #pragma unroll
     for (int i = 0; i < M::LOADS; ++i) {
         const int at = (wave + i * NW) * 1024 + lane * 16, at_row = at / ROW, piece = at % ROW / 16;
-        const int k_piece = piece ^ (at_row & (D / 8 - 1)), v_piece = piece ^ (D == 128 ? at_row & 3 : at_row >> 1 & 1) << 2;
+        const int k_piece = key_piece<D>(at_row, piece), v_piece = value_piece<D>(at_row, piece);
         from_row[i] = at_row;
         k_there[i] = 8 * k_piece < p.head_dim;
         v_there[i] = 8 * v_piece < p.head_dim;
@@ -478,77 +386,11 @@ template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW,
         bring_keys(tile, slot);
         bring_values(tile, slot);
     };
-    floatx16 o[ND] = {};
-    float m = -__builtin_inff(), l = 0;
     // a tile, or its first 32 keys where there are no others
     auto take = [&](int slot, uint64_t mask, auto halves) {
         constexpr int N = decltype(halves)::value;
-        const char* kt = lds + slot * M::SLOT + c * ROW;
-        floatx16 s[N] = {};
-#pragma unroll
-        for (int k = 0; k < NK; ++k) {
-            const char* at = kt + 16 * ((2 * k + h) ^ (c & (D / 8 - 1)));
-            const bf16x8 b = __builtin_bit_cast(bf16x8, q[k]);
-#pragma unroll
-            for (int t = 0; t < N; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(at + t * 32 * ROW), b, s[t], 0, 0, 0);
-        }
-        // reads two steps ahead of their products (left alone, the compiler puts each in front of its use)
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * N, 0);
-#pragma unroll
-        for (int k = 0; k < NK - 2; ++k) {
-            __builtin_amdgcn_sched_group_barrier(0x008, N, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, N, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, 2 * N, 0);
-        if (mask != (N == 2 ? ~0ull : 0xFFFFFFFFull)) {
-#pragma unroll
-            for (int t = 0; t < N; ++t) {
-                const uint32_t bits = (uint32_t)(mask >> (32 * t)) >> (4 * h);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const uint32_t in = __builtin_amdgcn_sbfe((int)bits, 8 * (i / 4) + (i & 3), 1);        // all bits or none
-                    s[t][i] = __uint_as_float((__float_as_uint(s[t][i]) & in) | (0xFF800000u & ~in));
-                }
-            }
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int i = 1; i < 16 * N; ++i) top = fmaxf(top, s[i / 16][i % 16]);
-        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-        top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * p.scale;
-        if (__any(top > m + 8.f)) {
-            top = fmaxf(m, top);
-            const float by = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.f : top));
-            m = top;
-            l *= by;
-#pragma unroll
-            for (int d = 0; d < ND; ++d) o[d] *= by;
-        }
-        const float base = m == -__builtin_inff() ? 0.f : m;
-#pragma unroll
-        for (int i = 0; i < 16 * N; ++i) {
-            s[i / 16][i % 16] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 16][i % 16], p.scale, -base));
-            l += s[i / 16][i % 16];
-        }
-        const char* vt = lds + slot * M::SLOT + M::PART + (4 * h + (lane >> 2 & 3)) * ROW + 32 * (lane >> 4 & 1) + 8 * (lane & 3);
-        const int turn = D == 128 ? lane >> 2 & 3 : lane >> 3 & 1;
-#pragma unroll
-        for (int k = 0; k < 2 * N; ++k) {
-            uint4 w;                                     // (rounded to bf16, as in Keys::add)
-            const int i = 8 * (k & 1);
-            w.x = pack_bf16x2(s[k / 2][i], s[k / 2][i + 1]);
-            w.y = pack_bf16x2(s[k / 2][i + 2], s[k / 2][i + 3]);
-            w.z = pack_bf16x2(s[k / 2][i + 4], s[k / 2][i + 5]);
-            w.w = pack_bf16x2(s[k / 2][i + 6], s[k / 2][i + 7]);
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                using Four = __attribute__((address_space(3))) shortx4*;
-                const char* at = vt + 16 * k * ROW + 64 * (d ^ turn);
-                const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four)(at + 8 * ROW));
-                const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, w), o[d], 0, 0, 0);
-            }
-        }
+        const char* at = lds + slot * M::SLOT;
+        run.template take<N>(at, at + M::PART, mask != (N == 2 ? ~0ull : 0xFFFFFFFFull), mask, p.scale, lane);
     };
     if (n_tiles) bring_keys(0, 0);
     if (MASK) {
@@ -558,7 +400,7 @@ template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW,
     if (n_tiles) bring_values(0, 0);
     // The queries are here, with the first tile: waited for in the loop, they would be together with the tiles that are on their way.
 #pragma unroll
-    for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(q[k].x), "+v"(q[k].y), "+v"(q[k].z), "+v"(q[k].w));
+    for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(run.q[k].x), "+v"(run.q[k].y), "+v"(run.q[k].z), "+v"(run.q[k].w));
     for (int i = 1; i < R - 1 && i < n_tiles; ++i) bring(i, i);
     for (int tile = 0, slot = 0, free = R - 1; tile < n_tiles; ++tile) {
         // (the tiles behind this one that are on their way: R - 2 but at the end)
@@ -576,20 +418,8 @@ template <int D, int NW, int R, bool MASK> __global__ __launch_bounds__(64 * NW,
         free = slot;                                     // (the slot that the tile before this one was in)
         slot = slot + 1 == R ? 0 : slot + 1;
     }
-    const auto sums = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-    l = __uint_as_float(sums[0]) + __uint_as_float(sums[1]);
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    bf16_t* out = static_cast<bf16_t*>(p.out) + q_row * p.out_stride + head * p.head_dim;
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; i += 8) {
-            // columns 8 h' .. + 7 of each 16: the lanes that share a row exchange halves
-            const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[d][i] * inv, o[d][i + 1] * inv), pack_bf16x2(o[d][i + 4] * inv, o[d][i + 5] * inv), false, false);
-            const auto y = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[d][i + 2] * inv, o[d][i + 3] * inv), pack_bf16x2(o[d][i + 6] * inv, o[d][i + 7] * inv), false, false);
-            const int column = 32 * d + 2 * i + 8 * h;
-            if (row < rows && column < p.head_dim) *reinterpret_cast<uint4*>(out + column) = make_uint4(x[0], y[0], x[1], y[1]);
-        }
+    const float l = run.sum(), m = run.m;
+    run.store(static_cast<bf16_t*>(p.out) + q_row * p.out_stride + head * p.head_dim, l == 0.f ? 0.f : 1.0f / l, row < rows, p.head_dim, lane);
     if (p.lse && row < rows && h == 0)
         p.lse[q_row * p.n_heads + head] = l == 0.f ? -__builtin_inff() : ((m == -__builtin_inff() ? 0.f : m) + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
