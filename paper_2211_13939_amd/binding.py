@@ -52,8 +52,8 @@ EXPORTS = (
 # every symbol include/tts_norm.h, tts_linear8.h and tts_cross.h declare
 OPERATOR_EXPORTS = tuple(f"tts_{op}_{call}" for op in ("norm", "linear8", "cross") for call in ("workspace_bytes", "create", "run", "destroy"))
 
-# every symbol include/tts_rotary.h and tts_cache.h declare
-PAST_EXPORTS = tuple(f"tts_{op}_{call}" for op in ("rotary", "cache") for call in ("workspace_bytes", "create", "run", "destroy"))
+# every symbol include/tts_rotary.h, tts_cache.h and tts_paged.h declare
+PAST_EXPORTS = tuple(f"tts_{op}_{call}" for op in ("rotary", "cache", "paged") for call in ("workspace_bytes", "create", "run", "destroy"))
 
 _fp = C.POINTER(C.c_float)
 _ip = C.POINTER(C.c_int)
@@ -147,6 +147,19 @@ class TtsCacheTensors(C.Structure):
     _fields_ = [("k", C.c_void_p), ("k_stride", C.c_longlong), ("v", C.c_void_p), ("v_stride", C.c_longlong), ("q", C.c_void_p), ("q_stride", C.c_longlong),
                 ("q_out", C.c_void_p), ("q_out_stride", C.c_longlong), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_longlong),
                 ("n_pages", C.c_int), ("table", C.c_void_p), ("table_rows", C.c_int), ("table_cols", C.c_int)]
+
+
+class TtsPagedConfig(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("n_heads", "n_kv_heads", "head_dim", "page_rows", "dtype", "causal")]
+
+
+class TtsPagedBatch(C.Structure):
+    _fields_ = [("n", C.c_int), ("q_len", _ip), ("own_len", _ip), ("table_row", _ip), ("prefix", _ip), ("n_prefixes", C.c_int), ("prefix_len", _ip), ("prefix_table_row", _ip)]
+
+
+class TtsPagedTensors(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_longlong), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_longlong), ("n_pages", C.c_int),
+                ("table", C.c_void_p), ("table_rows", C.c_int), ("table_cols", C.c_int), ("out", C.c_void_p), ("out_stride", C.c_longlong), ("lse", C.c_void_p), ("scale", C.c_float)]
 
 
 VOCODER_HOP = 256
@@ -255,12 +268,13 @@ def lib() -> C.CDLL:
     L.tts_cross_workspace_bytes.argtypes = [C.POINTER(TtsCrossConfig)]
     L.tts_cross_create.argtypes = [C.POINTER(TtsCrossConfig), vp, C.c_size_t, vp, C.POINTER(vp)]
     L.tts_cross_run.argtypes = [vp, C.POINTER(TtsCrossBatch), C.POINTER(TtsCrossTensors)]
-    for op, config, *args in (("rotary", TtsRotaryConfig, C.POINTER(TtsRotaryRows)), ("cache", TtsCacheConfig, C.POINTER(TtsCacheBatch), C.POINTER(TtsCacheTensors))):
+    for op, config, *args in (("rotary", TtsRotaryConfig, C.POINTER(TtsRotaryRows)), ("cache", TtsCacheConfig, C.POINTER(TtsCacheBatch), C.POINTER(TtsCacheTensors)),
+                             ("paged", TtsPagedConfig, C.POINTER(TtsPagedBatch), C.POINTER(TtsPagedTensors))):
         f = getattr(L, f"tts_{op}_workspace_bytes")
         f.restype, f.argtypes = C.c_size_t, [C.POINTER(config)]
         getattr(L, f"tts_{op}_create").argtypes = [C.POINTER(config), vp, C.c_size_t, vp, C.POINTER(vp)]
         getattr(L, f"tts_{op}_run").argtypes = [vp, *args]
-    for f in (L.tts_norm_destroy, L.tts_linear8_destroy, L.tts_cross_destroy, L.tts_rotary_destroy, L.tts_cache_destroy):
+    for f in (L.tts_norm_destroy, L.tts_linear8_destroy, L.tts_cross_destroy, L.tts_rotary_destroy, L.tts_cache_destroy, L.tts_paged_destroy):
         f.restype = None
         f.argtypes = [vp]
     _lib = L
@@ -1166,6 +1180,60 @@ class Cache(_Paged):
             a.q, a.q_stride = self._rows(q, "q", self._x_type, rows * of_q, rows)
             a.q_out, a.q_out_stride = self._rows(q_out, "q_out", self._pages_type, rows * of_q, rows)
         self._pages(a, k_pages, v_pages, table)
+        rc = self._run(self._handle, batch.c, a)
+        if rc:
+            _check(rc)
+
+
+def make_paged_config(n_heads: int, n_kv_heads: int, head_dim: int, page_rows: int, bf16: bool = False, causal: bool = True) -> TtsPagedConfig:
+    return TtsPagedConfig(int(n_heads), int(n_kv_heads), int(head_dim), int(page_rows), DTYPE_BF16 if bf16 else DTYPE_F32, int(bool(causal)))
+
+
+class PagedBatch:
+    """The numbers of a dynamic batch over a paged cache: of every request its queries, its own rows there, its row of the table and its prefix (-1, or None for all: none); of every
+    prefix its rows and its row of the table."""
+
+    def __init__(self, q_len, own_len, table_row, prefix=None, prefix_len=(), prefix_table_row=()):
+        n = len(q_len)
+        if len(own_len) != n or len(table_row) != n or (prefix is not None and len(prefix) != n):
+            raise ValueError("q_len, own_len, table_row and prefix have a value for each request")
+        if len(prefix_len) != len(prefix_table_row):
+            raise ValueError("prefix_len and prefix_table_row have a value for each prefix")
+        q, own, row, of, length, at = [None if v is None else CrossBatch._array(C.c_int, name, v) for name, v in (("q_len", q_len), ("own_len", own_len), ("table_row", table_row), ("prefix", prefix),
+                                                                                                            ("prefix_len", prefix_len), ("prefix_table_row", prefix_table_row))]
+        self.queries = sum(q)
+        self.c = TtsPagedBatch(n, q, own, row, of, len(length), length, at)      # (which keeps its arrays)
+
+
+class PagedAttention(_Paged):
+    """tts_paged_* calls: attention of a dynamic batch to its own rows, and to prefixes that requests share, in a paged cache."""
+
+    _name = "paged"
+
+    def __init__(self, cfg: TtsPagedConfig, stream=None, device: str = "cuda:0"):
+        where = self._setup(cfg, stream, device)
+        _check(lib().tts_paged_create(C.byref(cfg), *where))
+        self._setup_pages(cfg)
+        self._widths = (cfg.n_heads, cfg.n_heads * cfg.head_dim)
+
+    def batch(self, q_len, own_len, table_row, prefix=None, prefix_len=(), prefix_table_row=()) -> PagedBatch:
+        """A batch's numbers, for any number of calls."""
+        return PagedBatch(q_len, own_len, table_row, prefix, prefix_len, prefix_table_row)
+
+    def run_device(self, batch: PagedBatch, q, k_pages, v_pages, table, out, lse=None, scale: float = 0.0) -> None:
+        """q, out: CUDA [queries, n_heads, head_dim], rows any multiple of 8 elements apart; k_pages, v_pages: [pages, n_kv_heads, page_rows, head_dim], pages any multiple of 8 elements apart;
+        table: int32 [sequences, pages], other numbers than 0 .. pages - 1 for what is no page; lse: fp32 [queries, n_heads].  Queued on the object's stream; scale 0:
+        1 / sqrt(head_dim)."""
+        queries, (heads, of_q) = batch.queries, self._widths
+        a = TtsPagedTensors()
+        a.q, a.q_stride = self._rows(q, "q", self._pages_type, queries * of_q, queries)
+        a.out, a.out_stride = self._rows(out, "out", self._pages_type, queries * of_q, queries)
+        self._pages(a, k_pages, v_pages, table)
+        if lse is not None:
+            a.lse = self._at(lse, "lse", self._torch.float32, queries * heads)
+        a.scale = scale
+        if scale and not a.scale:
+            raise ValueError(f"a scale of {scale} is 0 in fp32")
         rc = self._run(self._handle, batch.c, a)
         if rc:
             _check(rc)

@@ -45,3 +45,50 @@ def places(table, table_row, first, n, page):
     """(page, row in it) of rows first .. first + n - 1 of a sequence."""
     j = np.arange(first, first + n)
     return table[table_row, j // page], j % page
+
+
+def paged(q, k_pages, v_pages, table, page, q_len, own_len, table_row, prefix=None, prefix_len=(), prefix_table_row=(), causal=True, scale=None):
+    """(out, lse, and what a derived tolerance takes: the sum of w |v|, the largest sum of |q| |k| of a row, times the scale)."""
+    _, heads, d = q.shape
+    n_pages, kv = k_pages.shape[:2]
+    group = heads // kv
+    scale = 1 / np.sqrt(d) if scale is None else scale
+    out, lse = np.zeros(q.shape), np.full(q.shape[:2], -np.inf)
+    mass, size = np.zeros(q.shape), np.zeros(q.shape[:2])
+    at = 0
+    for i, (n, m) in enumerate(zip(q_len, own_len)):
+        of = -1 if prefix is None else prefix[i]
+        pieces = ([(prefix_table_row[of], prefix_len[of], False)] if of >= 0 else []) + [(table_row[i], m, True)]
+        k, v, sees = [np.zeros((0, kv, d))], [np.zeros((0, kv, d))], [np.zeros((n, 0), bool)]
+        for row, length, own in pieces:
+            j = np.arange(length)
+            pg, off = places(table, row, 0, length, page) if length else (j, j)
+            there = (pg >= 0) & (pg < n_pages)
+            k.append(k_pages[pg[there], :, off[there]].astype(np.float64))
+            v.append(v_pages[pg[there], :, off[there]].astype(np.float64))
+            sees.append(j[there] <= m - n + np.arange(n)[:, None] if own and causal else np.ones((n, there.sum()), bool))
+        k, v, sees = np.concatenate(k), np.concatenate(v), np.concatenate(sees, 1)
+        for h in range(heads):
+            qq, kk, vv = q[at:at + n, h].astype(np.float64), k[:, h // group], v[:, h // group]
+            # (a key that nobody sees may hold anything, and one that some see is not used for the others)
+            any_sees = sees.any(0)
+            kk, vv, s_h = kk[any_sees], vv[any_sees], sees[:, any_sees]
+            if not len(kk) or not n:
+                continue
+            with np.errstate(invalid="ignore"):
+                s = np.where(s_h, scale * (qq @ kk.T), -np.inf)
+            top = s.max(1, keepdims=True)
+            none = np.isneginf(top[:, 0])
+            e = np.exp(s - np.where(np.isneginf(top), 0, top))
+            total = e.sum(1, keepdims=True)
+            w = e / np.where(total == 0, 1, total)
+            with np.errstate(invalid="ignore"):
+                odd = ~np.isfinite(vv).all(1)
+                out[at:at + n, h] = w[:, ~odd] @ vv[~odd]
+                for j in np.flatnonzero(odd):
+                    out[at:at + n, h][s_h[:, j]] += w[s_h[:, j], j: j + 1] * vv[j]
+                mass[at:at + n, h] = w[:, ~odd] @ np.abs(vv[~odd])
+                lse[at:at + n, h] = np.where(none, -np.inf, np.where(none, 0, top[:, 0]) + np.log(np.where(none, 1, total[:, 0])))
+                size[at:at + n, h] = np.where(s_h, scale * (np.abs(qq) @ np.abs(kk).T), 0).max(1)
+        at += n
+    return out, lse, mass, size

@@ -1,4 +1,4 @@
-"""The host code of a decoder block's own past (tts_rotary, tts_cache) without a GPU: what the headers declare is exported, what they do not allow is refused before anything is
+"""The host code of a decoder block's own past (tts_rotary, tts_cache, tts_paged) without a GPU: what the headers declare is exported, what they do not allow is refused before anything is
 launched, failing HIP calls come back as errors, frequencies hold what the definition says."""
 import ctypes as C
 import os
@@ -12,7 +12,7 @@ from paper_2211_13939_amd import binding
 from tests import past_ref as ref
 from tests.test_operators_host import HIP, INVAL, ROOT, UNSUPPORTED, Made
 
-OPS = ("rotary", "cache")
+OPS = ("rotary", "cache", "paged")
 
 
 def test_library_exports_every_declared_operator():
@@ -20,7 +20,7 @@ def test_library_exports_every_declared_operator():
     for op in OPS:
         text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", f"tts_{op}.h")).read(), flags=re.S)
         names |= set(re.findall(rf"\b(tts_{op}_(?!angles|config|rows|batch|tensors)\w+)\s*\(", text))
-    assert names == {n for n in binding.PAST_EXPORTS if n.split("_")[1] in OPS}
+    assert names == set(binding.PAST_EXPORTS)
     for n in names:
         assert hasattr(binding.lib(), n), n
 
@@ -58,7 +58,15 @@ def test_configurations_without_gpu():
         for k, v in change.items():
             setattr(c, k, v)
         assert L.tts_cache_workspace_bytes(C.byref(c)) == 0 and L.tts_last_error(), change
-    assert L.tts_rotary_workspace_bytes(None) == 0 and L.tts_cache_workspace_bytes(None) == 0
+    assert L.tts_paged_workspace_bytes(C.byref(binding.make_paged_config(8, 2, 64, 16))) > 0
+    for change in (dict(n_heads=0), dict(n_heads=257), dict(n_kv_heads=0), dict(n_kv_heads=3), dict(n_kv_heads=16), dict(head_dim=0), dict(head_dim=12), dict(head_dim=136), dict(page_rows=8),
+                   dict(page_rows=24), dict(page_rows=2048), dict(dtype=2), dict(causal=2)):
+        c = binding.make_paged_config(8, 2, 64, 16)
+        for k, v in change.items():
+            setattr(c, k, v)
+        assert L.tts_paged_workspace_bytes(C.byref(c)) == 0 and L.tts_last_error(), change
+    for op in OPS:
+        assert getattr(L, f"tts_{op}_workspace_bytes")(None) == 0
 
 
 @pytest.fixture(scope="module")
@@ -69,7 +77,8 @@ def lib(tmp_path_factory):
                     os.path.join(ROOT, "tests", "fake_past.cpp")] + [os.path.join(csrc, f"{op}.cpp") for op in OPS] + ["-o", out], check=True)
     L = C.CDLL(out)
     L.tts_last_error.restype = C.c_char_p
-    L.past_append_k.restype = C.c_longlong
+    L.past_append_k.restype = L.past_rows.restype = C.c_longlong
+    L.past_wrong.restype = C.c_char_p
     for op in OPS:
         getattr(L, f"tts_{op}_workspace_bytes").restype = C.c_size_t
         f = getattr(L, f"tts_{op}_destroy")
@@ -182,7 +191,87 @@ def test_cache_refuses(lib):
     none.close()
 
 
+def _paged(lib, m, q_len=(2, 0, 3), own=(5, 4, 0), table_row=(0, 1, 2), prefix=(0, -1, 1), lens=(7, 9), rows=(3, 4), n=None, null=None, **change):
+    b = binding.PagedBatch(list(q_len), list(own), list(table_row), None if prefix is None else list(prefix), list(lens), list(rows))
+    if n is not None:
+        b.c.n = n
+    if null:
+        setattr(b.c, null, C.POINTER(C.c_int)())
+    t = binding.TtsPagedTensors(q=1 << 20, k_pages=2 << 20, v_pages=3 << 20, out=4 << 20, table=5 << 20, lse=6 << 20, n_pages=7, table_rows=5, table_cols=4)
+    for key, v in change.items():
+        setattr(b.c if key == "n_prefixes" else t, key, v)
+    before = lib.fake_launches()
+    rc = lib.tts_paged_run(m.h, C.byref(b.c), C.byref(t))
+    assert (lib.fake_launches() > before) == (rc == 0 and sum(q_len) > 0)
+    assert lib.past_wrong() == b""
+    return rc
+
+
+def test_paged_refuses(lib):
+    lib.past_reset()
+    m = Made(lib, "paged", binding.make_paged_config(8, 2, 40, 32, True))
+    wide = binding.make_paged_config(8, 2, 136, 32)
+    assert lib.tts_paged_create(C.byref(wide), None, C.c_size_t(0), None, C.byref(C.c_void_p())) == UNSUPPORTED
+
+    def run(**change):
+        return _paged(lib, m, **change)
+
+    assert run() == 0 and lib.fake_requests_seen() == 2 and lib.past_rows() == 20 and lib.past_pools() == 2 and lib.past_joins() == 1          # a request without queries is left out
+    lib.past_reset()
+    assert run(prefix=None) == 0 and lib.past_pools() == 0 and lib.past_joins() == 0
+    assert run(prefix=(-1, 0, -1)) == 0 and lib.past_pools() == 0                                                                               # nobody's prefix is not read
+    assert run(q_len=(0, 0, 0), q=None, out=None, k_pages=None, v_pages=None, table=None) == 0
+    assert run(own=(0, 0, 0), table_row=(9, -1, 5), lens=(0, 0), rows=(-1, 99), k_pages=None, v_pages=None, table=None) == 0 and lib.past_pools() == 0
+    assert run(prefix=None, lens=(), rows=()) == 0 and run(lse=None) == 0 and run(own=(128, 1, 97)) == 0 and run(scale=0.5) == 0
+    assert run(page_stride=2 * 32 * 40 + 8, q_stride=328, out_stride=1 << 40) == 0
+    for change in (dict(n=0), dict(n=-1), dict(null="q_len"), dict(null="own_len"), dict(null="table_row"), dict(null="prefix_len"), dict(null="prefix_table_row"), dict(q_len=(-1, 0, 0)),
+                   dict(q_len=((1 << 24) + 1, 0, 0)), dict(own=(-1, 0, 0)), dict(own=((1 << 24) + 1, 0, 0)), dict(own=(129, 0, 0)), dict(table_row=(5, 1, 2)), dict(table_row=(-1, 1, 2)),
+                   dict(prefix=(2, 0, 0)), dict(prefix=(-2, 0, 0)), dict(lens=(-1, 9)), dict(lens=(7, 129)), dict(lens=(7, (1 << 24) + 1)), dict(rows=(3, 5)), dict(rows=(-1, 4)),
+                   dict(n_prefixes=-1), dict(n_prefixes=1025), dict(n_prefixes=0), dict(q=None), dict(out=None), dict(k_pages=None), dict(v_pages=None), dict(table=None), dict(n_pages=0), dict(table_rows=0),
+                   dict(table_cols=0), dict(q_stride=319), dict(q_stride=312), dict(out_stride=-320), dict(out_stride=(1 << 40) + 8), dict(page_stride=2552), dict(page_stride=2564), dict(q=(1 << 20) + 8),
+                   dict(k_pages=(2 << 20) + 8), dict(v_pages=(3 << 20) + 4), dict(out=(4 << 20) + 8), dict(table=(5 << 20) + 2), dict(lse=(6 << 20) + 2), dict(scale=-1.0), dict(scale=float("nan")),
+                   dict(scale=float("inf")), dict(scale=2.4e38), dict(q_len=[1] * 1025, own=[0] * 1025, table_row=[0] * 1025, prefix=None),
+                   dict(q_len=[1 << 24] * 129, own=[0] * 129, table_row=[0] * 129, prefix=None), dict(q_len=[1 << 24, 1], own=[0] * 2, table_row=[0] * 2, prefix=None)):
+        assert run(**change) == INVAL, change
+        assert lib.tts_last_error()
+    assert run(scale=2.3e38) == 0 and run(q_len=[1 << 24], own=[1], table_row=[0], prefix=None) == 0
+    assert lib.tts_paged_run(None, None, None) == INVAL and lib.tts_paged_run(m.h, None, None) == INVAL
+    lib.fake_fail(b"launch")
+    assert _paged(lib, m, q_len=(0, 0, 0)) == 0
+    b, t = binding.PagedBatch([1], [1], [0]), binding.TtsPagedTensors(q=1 << 20, k_pages=2 << 20, v_pages=3 << 20, out=4 << 20, table=5 << 20, n_pages=7, table_rows=5, table_cols=4)
+    assert lib.tts_paged_run(m.h, C.byref(b.c), C.byref(t)) == HIP
+    lib.past_reset()
+    m.close()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("heads,kv,d", [(1, 1, 64), (8, 8, 64), (32, 8, 128), (16, 4, 128), (256, 256, 8), (256, 1, 128)])
+def test_plans_of_attention(lib, heads, kv, d, bf16):
+    """Launches of all kinds of batches: every request in one of them, parts that cover their sequences, parts that fit in the arena and are joined ahead of the next launch."""
+    rng = np.random.default_rng(heads + d)
+    m = Made(lib, "paged", binding.make_paged_config(heads, kv, d, 16, bf16))
+    for n in (1, 2, 16, 17, 64, 128, 129, 500, 1024):
+        for q_hi in (1, 3, 40, 700):
+            for own_hi in (0, 30, 500, 20000):
+                for prefixes, pre_hi in ((0, 0), (1, 100), (1, 16000), (3, 1000), (50, 300)):
+                    q_len = [int(v) for v in rng.integers(0 if n > 4 else 1, q_hi + 1, n)]
+                    if sum((q * (heads // kv) + 15) // 16 * kv for q in q_len) > 1 << 23:
+                        continue
+                    own = [int(v) for v in rng.integers(0, own_hi + 1, n)]
+                    prefix = [int(v) for v in rng.integers(-1, prefixes, n)]
+                    lens = [int(v) for v in rng.integers(0, pre_hi + 1, prefixes)]
+                    lib.past_reset()
+                    assert _paged(lib, m, q_len, own, [0] * n, prefix, lens, [1] * prefixes, table_cols=2000) == 0
+                    assert lib.fake_requests_seen() == sum(q > 0 for q in q_len) and lib.past_rows() == sum(q_len) * (heads // kv), (n, q_hi, own_hi, prefixes)
+    m.close()
+
+
 def test_numbers_that_their_types_do_not_hold():
+    for args in (([1], [1 << 32], [0]), ([1 << 32], [1], [0]), ([1], [1], [-(1 << 32)]), ([1], [1], [0], [1 << 31]), ([1], [1], [0], [0], [1 << 32], [0]), ([1], [1], [0], [0], [1, 2], [0]),
+                 ([1], [1, 2], [0]), ([1], [1], [0], [0, 1], [1], [1])):
+        with pytest.raises(ValueError):
+            binding.PagedBatch(*args)
+    assert binding.PagedBatch([1, 2], [3, 4], [0, 1], [0, -1], [5], [2]).queries == 3
     with pytest.raises(ValueError):
         binding.CacheBatch([1], [1 << 32], [0])
     with pytest.raises(ValueError):
