@@ -163,8 +163,13 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
                 const int height = plan_paged_many(a, p->n_cu);
                 e = launch_paged_many(a, height, p->stream);
             } else {
-                plan_paged_few(a, bf16 ? 2 : 4, p->n_cu);
+                const int height = a.pooled && bf16 ? paged_pool_height(a, p->n_cu) : 0;
+                plan_paged_few(a, bf16 ? 2 : 4, p->n_cu, a.pooled && !height);
                 e = launch_paged_few(a, bf16, p->stream);
+                if (e == hipSuccess && height) {
+                    plan_paged_pools(a, height, p->n_cu);
+                    e = launch_paged_many(a, height, p->stream);
+                }
                 if (e == hipSuccess && ((a.pooled && a.n_pools) || a.share)) e = launch_paged_join(a, bf16, p->stream);
             }
             clear();

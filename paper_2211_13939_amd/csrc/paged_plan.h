@@ -17,25 +17,24 @@ inline bool paged_many(long long few_tiles, int n_cu) { return 2 * few_tiles >= 
 // Room for parts, in parts of 16 rows: more than a launch is split into, and enough for a tile of each of its requests and key heads beside their prefixes'.
 inline int paged_room(int n_kv_heads) { return 4096 + PAGED_BATCH * n_kv_heads; }
 
-// The split of a launch's sequences (tiles of 16 rows) into parts of one length: shortest that `most` workgroups go through at once.  0: none.
+// The split of a launch's sequences into parts of one length: shortest that `most` workgroups go through at once.  0: none.
 template <typename Items> int paged_share(double keys, long long tiles, int longest, int most, Items items)
 {
     if (2 * tiles > most) return 0;
     double share = std::max({keys / (most - 0.5 * tiles), (double)longest / PAGED_MAX_SPLITS, 128.0});
-    auto whole = [](double s) { return ((int)std::ceil(s) + 31) / 32 * 32; };
+    auto whole = [](double s) { return ((int)std::ceil(s) + 63) / 64 * 64; };      // (tiles of 64 keys, steps of 32)
     while (share < longest && items(whole(share)) > most) share *= 1.0625;
     if (share >= longest) return 0;
     const int parts = (longest - 1) / whole(share) + 1, even = whole((longest - 1) / parts + 1);
     return items(even) <= most ? even : whole(share);
 }
 
-// Requests of few rows, gathered: tiles and parts.  n_cu: compute units.
-inline void plan_paged_few(PagedArgs& a, int element_bytes, int n_cu)
+// Requests of few rows, gathered: tiles and parts.  n_cu: compute units; pools: whether prefixes' tiles are of 16 rows, too, in the same launch.
+inline void plan_paged_few(PagedArgs& a, int element_bytes, int n_cu, bool pools)
 {
     const int d = paged_width(a.head_dim);
     auto tiles_of = [](int rows) { return (long long)(rows + 15) / 16; };
     auto rows_of = [&](int i) { return a.row[i + 1] - a.row[i]; };
-    auto pool_rows = [&](int g) { return a.row[a.pool[g].end] - a.row[a.pool[g].begin]; };
     int longest = 0;
     long long tiles = 0;
     double keys = 0;
@@ -45,8 +44,8 @@ inline void plan_paged_few(PagedArgs& a, int element_bytes, int n_cu)
         longest = std::max(longest, len);
     };
     for (int i = 0; i < a.n; ++i) more(tiles_of(rows_of(i)), paged_len(a, i));
-    if (a.pooled)
-        for (int g = 0; g < a.n_pools; ++g) more(tiles_of(pool_rows(g)), a.pool[g].len);
+    if (pools)
+        for (int g = 0; g < a.n_pools; ++g) more(tiles_of(a.row[a.pool[g].end] - a.row[a.pool[g].begin]), a.pool[g].len);
     auto cut = [&](int share) {
         long long items = 0;
         for (int i = 0; i < a.n; ++i) {
@@ -54,10 +53,10 @@ inline void plan_paged_few(PagedArgs& a, int element_bytes, int n_cu)
             items += tiles_of(rows_of(i)) * a.n_kv_heads * paged_parts(paged_len(a, i), share);
         }
         a.pool_first = (int)items;
-        if (a.pooled)
+        if (pools)
             for (int g = 0; g < a.n_pools; ++g) {
                 a.pool[g].first = (int)items;
-                items += tiles_of(pool_rows(g)) * a.n_kv_heads * paged_parts(a.pool[g].len, share);
+                items += tiles_of(a.row[a.pool[g].end] - a.row[a.pool[g].begin]) * a.n_kv_heads * paged_parts(a.pool[g].len, share);
             }
         return items;
     };
@@ -68,7 +67,7 @@ inline void plan_paged_few(PagedArgs& a, int element_bytes, int n_cu)
     const bool alike = longest * (double)tiles <= 1.25 * keys;
     const int most = (d == 128 ? 2 : alike ? 4 : 8) * n_cu;
     a.share = 0;
-    if ((a.pooled && a.n_pools) || here / rate > 1.1 * all / 5.1e6 + 5) a.share = paged_share(keys, tiles, longest, most, cut);
+    if ((pools && a.n_pools) || here / rate > 1.1 * all / 5.1e6 + 5) a.share = paged_share(keys, tiles, longest, most, cut);
     a.pool_share = a.share;
     a.pool_height = PAGED_FEW_ROWS;
     a.items = (int)cut(a.share);
@@ -94,6 +93,49 @@ template <typename Entry> int plan_runs(PagedArgs& a, int first, int n, Entry en
     }
     for (; x <= 8; ++x) a.start[x] = at;
     return at;
+}
+
+// Prefixes' tiles of many rows, in a launch of their own behind that of the requests' own rows.
+inline int pool_rows(const PagedArgs& a, int g) { return a.row[a.pool[g].end] - a.row[a.pool[g].begin]; }
+// Their height, 0: tiles of 16 serve (few rows of each, short ones, or no room for the parts).
+inline int paged_pool_height(const PagedArgs& a, int n_cu)
+{
+    int most = 0;
+    for (int g = 0; g < a.n_pools; ++g)
+        if (a.pool[g].len >= 512) most = std::max(most, pool_rows(a, g));
+    if (most < 64) return 0;
+    const int height = most > 64 ? 128 : 64;
+    long long tiles = 0, own = 0;
+    for (int g = 0; g < a.n_pools; ++g) tiles += (pool_rows(a, g) + height - 1) / height * a.n_kv_heads;
+    for (int i = 0; i < a.n; ++i) own += (a.row[i + 1] - a.row[i] + 15) / 16 * a.n_kv_heads;
+    return tiles * height <= (paged_room(a.n_kv_heads) - std::max<long long>(own, 8 * n_cu)) * PAGED_FEW_ROWS ? height : 0;
+}
+inline void plan_paged_pools(PagedArgs& a, int height, int n_cu)
+{
+    const int d = paged_width(a.head_dim);
+    auto tiles_of = [&](int g) { return (pool_rows(a, g) + height - 1) / height * a.n_kv_heads; };
+    double keys = 0;
+    long long tiles = 0;
+    int longest = 0;
+    for (int g = 0; g < a.n_pools; ++g) {
+        keys += (double)tiles_of(g) * a.pool[g].len;
+        tiles += tiles_of(g);
+        longest = std::max(longest, a.pool[g].len);
+    }
+    const long long room = ((long long)paged_room(a.n_kv_heads) - a.pool_first) * PAGED_FEW_ROWS / height;
+    auto cut = [&](int share) {
+        long long items = 0;
+        for (int g = 0; g < a.n_pools; ++g) {
+            a.pool[g].first = a.pool_first + (int)items;
+            items += (long long)tiles_of(g) * paged_parts(a.pool[g].len, share);
+        }
+        return items;
+    };
+    a.pool_height = height;
+    a.pool_share = paged_share(keys, tiles, longest, (int)std::min<long long>(room, (d == 128 ? 2 : 3) * n_cu), cut);
+    a.items = a.pool_first + (int)cut(a.pool_share);
+    a.pool_parts = a.parts + (size_t)a.pool_first * paged_part_floats(PAGED_FEW_ROWS, d);
+    plan_runs(a, a.pool_first, a.n_pools, [&](int g) { return std::pair<int, double>(tiles_of(g) * paged_parts(a.pool[g].len, a.pool_share), a.pool_share ? a.pool_share : a.pool[g].len); });
 }
 
 // Requests of many rows, gathered: the height of a tile.

@@ -8,13 +8,13 @@ namespace {
 std::string wrong;
 int few = 0, many = 0, joins = 0, pools = 0, split = 0, last_height = 0;
 long long rows_seen = 0;
-bool parts_pending = false;
+bool parts_pending = false, pools_pending = false;
 void expect(bool ok, const char* what)
 {
     if (!ok && wrong.empty()) wrong = what;
 }
 // Every tile of a launch: entries' tiles follow each other, parts cover their sequence, and what is written apart fits in the arena.
-void look_at(const tts::PagedArgs& a, int height, bool all_at_once)
+void look_at(const tts::PagedArgs& a, int height, bool requests, bool prefixes)
 {
     using namespace tts;
     const long long room = (long long)paged_room(a.n_kv_heads) * paged_part_floats(16, paged_width(a.head_dim));
@@ -22,7 +22,7 @@ void look_at(const tts::PagedArgs& a, int height, bool all_at_once)
     long long at = 0;
     bool apart = false;
     expect(a.n >= 1 && a.n <= PAGED_BATCH && a.n_pools <= PAGED_POOLS && a.row[0] == 0, "numbers of the launch");
-    for (int i = 0; i < a.n; ++i) {
+    for (int i = 0; requests && i < a.n; ++i) {
         const int rows = a.row[i + 1] - a.row[i], len = paged_len(a, i), parts = paged_parts(len, a.share), g = a.pool_of[i];
         expect(rows > 0 && rows % group == 0 && (!a.each || rows == a.each), "rows of a request");
         expect(g < a.n_pools && (g < 0 || (a.pool[g].begin <= i && i < a.pool[g].end)), "a request's prefix");
@@ -33,8 +33,9 @@ void look_at(const tts::PagedArgs& a, int height, bool all_at_once)
         split += parts > 1;
         rows_seen += rows;
     }
+    if (!requests) at = a.pool_first;
     expect(at == a.pool_first && (!apart || at * (long long)paged_part_floats(height, paged_width(a.head_dim)) <= room), "room for requests' parts");
-    if (a.pooled)
+    if (prefixes)
         for (int g = 0; g < a.n_pools; ++g) {
             const PagedPool& o = a.pool[g];
             const int parts = paged_parts(o.len, a.pool_share);
@@ -44,10 +45,11 @@ void look_at(const tts::PagedArgs& a, int height, bool all_at_once)
             split += parts > 1;
         }
     const long long pool_floats = (at - a.pool_first) * (long long)paged_part_floats(a.pool_height, paged_width(a.head_dim));
-    expect(!a.pooled || !a.n_pools || (a.pool_parts - a.parts >= a.pool_first * (long long)paged_part_floats(16, paged_width(a.head_dim)) && a.pool_parts - a.parts + pool_floats <= room), "room for prefixes' parts");
-    expect(a.items == (all_at_once ? at : a.pool_first), "tiles of the launch");
-    pools += a.pooled ? a.n_pools : 0;
-    parts_pending = apart || (a.pooled && a.n_pools);
+    expect(!prefixes || (a.pool_parts - a.parts >= a.pool_first * (long long)paged_part_floats(16, paged_width(a.head_dim)) && a.pool_parts - a.parts + pool_floats <= room), "room for prefixes' parts");
+    expect(a.items == at, "tiles of the launch");
+    pools += prefixes ? a.n_pools : 0;
+    parts_pending |= apart || prefixes;
+    pools_pending = requests && !prefixes && a.pooled && a.n_pools;
 }
 tts::RotaryArgs rotary;
 tts::AppendArgs append;
@@ -78,7 +80,7 @@ hipError_t launch_paged_few(const PagedArgs& a, bool, hipStream_t)
     ++few;
     requests_seen += a.n;
     expect(!parts_pending, "parts that were not joined");
-    look_at(a, PAGED_FEW_ROWS, a.pool_height == PAGED_FEW_ROWS);
+    look_at(a, PAGED_FEW_ROWS, true, a.pooled && a.n_pools && a.items > a.pool_first);
     return call("launch");
 }
 hipError_t launch_paged_many(const PagedArgs& a, int height, hipStream_t)
@@ -86,10 +88,15 @@ hipError_t launch_paged_many(const PagedArgs& a, int height, hipStream_t)
     ++launches;
     ++many;
     last_height = height;
-    requests_seen += a.n;
-    expect(!parts_pending, "parts that were not joined");
-    look_at(a, height, true);
-    expect(a.start[0] == 0 && a.start[8] == a.items, "shares of the XCDs");
+    if (a.pooled) {
+        expect(pools_pending && a.pool_height == height, "prefixes behind their requests");
+        look_at(a, height, false, true);
+    } else {
+        requests_seen += a.n;
+        expect(!parts_pending, "parts that were not joined");
+        look_at(a, height, true, false);
+    }
+    expect(a.start[0] == (a.pooled ? a.pool_first : 0) && a.start[8] == a.items, "shares of the XCDs");
     for (int i = 0; i < 8; ++i) expect(a.start[i] <= a.start[i + 1], "shares in order");
     return call("launch");
 }
@@ -97,6 +104,7 @@ hipError_t launch_paged_join(const PagedArgs&, bool, hipStream_t)
 {
     ++launches;
     ++joins;
+    expect(!pools_pending, "prefixes that were not read");
     parts_pending = false;
     return call("launch");
 }
@@ -108,7 +116,7 @@ void past_reset()
     fake_reset();
     append_rows = few = many = joins = pools = split = last_height = 0;
     rows_seen = 0;
-    parts_pending = false;
+    parts_pending = pools_pending = false;
     wrong.clear();
 }
 const char* past_wrong()
