@@ -35,13 +35,27 @@ int check_sequence(const char* what, int i, int len, int table_row, int page_shi
     return TTS_OK;
 }
 
-enum class Form { FEW, WHOLE, MANY };                // few rows, prefixes apart; tiles of 16 over whole sequences; tiles of 128 or 256
+struct Layout { size_t parts, arrived, total; };
+size_t part_floats(const tts_paged_config& c) { return paged_room(c.n_kv_heads) * paged_part_floats(PAGED_FEW_ROWS, paged_width(c.head_dim)); }
+size_t arrived_bytes(const tts_paged_config& c) { return (size_t)paged_room(c.n_kv_heads) * PAGED_FEW_ROWS * 4; }
+Layout layout_of(const tts_paged_config& c)
+{
+    Layout l;
+    Carver a;
+    l.parts = a.take(part_floats(c) * 4);
+    l.arrived = a.take(arrived_bytes(c));
+    l.total = a.off;
+    return l;
+}
+
+enum class Form { FEW, WHOLE, MANY };                // tiles of 16 rows, prefixes apart if that pays; tiles of 16 over whole sequences; tiles of 128 or 256
 
 }  // namespace
 
 struct tts_paged {
     tts_paged_config cfg;
     float* parts = nullptr;              // device
+    int* arrived = nullptr;
     hipStream_t stream = nullptr;
     int device = 0, n_cu = 0;
 };
@@ -49,9 +63,7 @@ struct tts_paged {
 extern "C" size_t tts_paged_workspace_bytes(const tts_paged_config* cfg)
 {
     if (check(cfg) != TTS_OK) return 0;
-    Carver a;
-    a.take(paged_room(cfg->n_kv_heads) * paged_part_floats(PAGED_FEW_ROWS, paged_width(cfg->head_dim)) * 4);
-    return a.off;
+    return layout_of(*cfg).total;
 }
 
 extern "C" int tts_paged_create(const tts_paged_config* cfg, void* dev_arena, size_t arena_bytes, void* hip_stream, tts_paged** out)
@@ -61,15 +73,18 @@ extern "C" int tts_paged_create(const tts_paged_config* cfg, void* dev_arena, si
     int rc = check(cfg);
     if (rc) return rc;
     int device = 0, n_cu = 0;
-    if ((rc = check_arena(dev_arena, arena_bytes, tts_paged_workspace_bytes(cfg), &device))) return rc;
+    const Layout lay = layout_of(*cfg);
+    if ((rc = check_arena(dev_arena, arena_bytes, lay.total, &device))) return rc;
     OnDevice on(device);
     HIP_TRY(on.err);
     HIP_TRY(allow_paged());
+    HIP_TRY(fill_now((char*)dev_arena + lay.arrived, 0, arrived_bytes(*cfg)));
     HIP_TRY(hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, device));
     tts_paged* p = new (std::nothrow) tts_paged();
     if (!p) return fail(TTS_E_INVAL, "out of host memory");
     p->cfg = *cfg;
-    p->parts = (float*)dev_arena;
+    p->parts = (float*)((char*)dev_arena + lay.parts);
+    p->arrived = (int*)((char*)dev_arena + lay.arrived);
     p->stream = (hipStream_t)hip_stream;
     p->device = device;
     p->n_cu = n_cu;
@@ -119,7 +134,9 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
     a.q = t->q; a.k_pages = t->k_pages; a.v_pages = t->v_pages; a.out = t->out;
     a.table = t->table;
     a.lse = t->lse;
-    a.parts = p->parts;
+    a.parts = a.pool_parts = p->parts;
+    a.part_floats = (int)part_floats(c);
+    a.arrived = p->arrived;
     a.scale = scale;
     a.n_heads = c.n_heads; a.n_kv_heads = c.n_kv_heads; a.head_dim = c.head_dim;
     a.n_pages = t->n_pages; a.table_cols = t->table_cols; a.page_shift = shift;
@@ -137,7 +154,7 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
     for (int i = 0; i < b->n; ++i) order[count[prefix_of(i) + 1]++] = i;
     auto rows_of = [&](int i) { return (long long)b->q_len[i] * group; };
     auto form_of = [&](int i) {
-        return rows_of(i) < PAGED_MANY_ROWS ? Form::FEW : any_many ? Form::MANY : Form::WHOLE;
+        return any_many && rows_of(i) >= PAGED_MANY_ROWS ? Form::MANY : rows_of(i) < PAGED_MANY_ROWS || few_tiles <= 1024 ? Form::FEW : Form::WHOLE;
     };
     OnDevice on(p->device);
     HIP_TRY(on.err);
@@ -154,23 +171,46 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
         };
         auto launch = [&]() -> hipError_t {
             if (!a.n) return hipSuccess;
-            a.pooled = form == Form::FEW;
+            a.pooled = false;
+            a.rows = a.row[a.n];
+            a.by_group = (long long)a.rows * group <= 1LL << 32 || (group & (group - 1)) == 0 ? by_of(group) : NOT_BY;
             a.each = a.row[1];
-            for (int i = 1; i < a.n; ++i)
-                if (a.row[i + 1] - a.row[i] != a.each) a.each = 0;
+            a.q_first = a.req[0].q_row;
+            for (int i = 1; i < a.n; ++i) {
+                if (a.row[i + 1] - a.row[i] != a.row[1]) a.each = 0;
+                if (a.req[i].q_row != a.req[0].q_row + a.row[i] / group) a.q_first = -1;
+            }
             hipError_t e;
             if (form == Form::MANY) {
                 const int height = plan_paged_many(a, p->n_cu);
                 e = launch_paged_many(a, height, p->stream);
             } else {
-                const int height = a.pooled && bf16 ? paged_pool_height(a, p->n_cu) : 0;
-                plan_paged_few(a, bf16 ? 2 : 4, p->n_cu, a.pooled && !height);
-                e = launch_paged_few(a, bf16, p->stream);
+                // prefixes ahead of each request's own rows, as tiles of their own beside them, or as a launch of larger ones
+                const int bytes = bf16 ? 2 : 4;
+                double unique = 0;
+                for (int i = 0; i < a.n; ++i) unique += own_len_of(a.req[i]);
+                for (int g = 0; g < a.n_pools; ++g) unique += a.pool[g].len;
+                unique *= 2.0 * c.n_kv_heads * c.head_dim * bytes;
+                PagedCut cut = paged_cut(a, PagedPools::NONE, bytes, p->n_cu, unique, room);
+                int height = 0;
+                if (form == Form::FEW && a.n_pools) {
+                    const PagedCut tiles = paged_cut(a, PagedPools::TILES, bytes, p->n_cu, unique, room);
+                    if (tiles.ns < cut.ns) cut = tiles;
+                    height = bf16 ? paged_pool_height(a, p->n_cu) : 0;
+                    if (height) {
+                        PagedCut apart = paged_cut(a, PagedPools::APART, bytes, p->n_cu, unique, 8 * p->n_cu);
+                        apart.ns += paged_pools_ns(a, height, p->n_cu);
+                        if (apart.ns < cut.ns) cut = apart;
+                        else height = 0;
+                    }
+                }
+                plan_paged_few(a, cut);
+                e = launch_paged_few(a, bf16, p->n_cu, p->stream);
                 if (e == hipSuccess && height) {
                     plan_paged_pools(a, height, p->n_cu);
                     e = launch_paged_many(a, height, p->stream);
                 }
-                if (e == hipSuccess && ((a.pooled && a.n_pools) || a.share)) e = launch_paged_join(a, bf16, p->stream);
+                if (e == hipSuccess && !a.join && ((a.pooled && a.n_pools) || a.share)) e = launch_paged_join(a, bf16, p->stream);
             }
             clear();
             return e;
@@ -188,8 +228,7 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
                 a.pool[a.n_pools++] = PagedPool{b->prefix_table_row[prefix], b->prefix_len[prefix], a.n, a.n, 0};
                 last_prefix = prefix;
             }
-            a.req[a.n] = PagedReq{b->own_len[i], b->table_row[i], q_row[i], 0};
-            a.pool_of[a.n] = (signed char)(prefix >= 0 ? a.n_pools - 1 : -1);
+            a.req[a.n] = PagedReq{(unsigned)b->own_len[i] | (unsigned)(prefix >= 0 ? a.n_pools : 0) << 25, b->table_row[i], q_row[i], 0};
             a.row[a.n + 1] = a.row[a.n] + (int)rows_of(i);
             ++a.n;
             if (prefix >= 0) a.pool[a.n_pools - 1].end = a.n;

@@ -17,61 +17,127 @@ inline bool paged_many(long long few_tiles, int n_cu) { return 2 * few_tiles >= 
 // Room for parts, in parts of 16 rows: more than a launch is split into, and enough for a tile of each of its requests and key heads beside their prefixes'.
 inline int paged_room(int n_kv_heads) { return 4096 + PAGED_BATCH * n_kv_heads; }
 
-// The split of a launch's sequences into parts of one length: shortest that `most` workgroups go through at once.  0: none.
-template <typename Items> int paged_share(double keys, long long tiles, int longest, int most, Items items)
+// How requests of few rows, gathered, are cut into tiles of 16 rows and parts of their keys.
+enum class PagedPools { NONE, TILES, APART };        // prefixes: ahead of their requests' own rows; tiles of theirs in the same launch; a launch of their own behind this
+struct PagedCut {
+    PagedPools pools;
+    int share;                           // length of a part, 0: whole sequences
+    double ns;                           // what it should take
+};
+// A workgroup's way from its launch to its first keys and from the last ones to its results (3.2 us measured, with one step); a step of its waves: the matrix pipe's (two waves a SIMD take turns), or its
+// keys' and values' way, by latency: 45 GB/s to a workgroup of four waves from the last-level cache, 28 from memory, 70 and 43 to one of eight.
+struct PagedCosts {
+    int keys, held;                      // of a wave's step; workgroups of four waves that a compute unit holds
+    double step[2];                      // ns, of workgroups of four waves and of eight
+};
+constexpr double PAGED_START = 3500;
+inline PagedCosts paged_costs(int d, int element_bytes, bool far)
 {
-    if (2 * tiles > most) return 0;
-    double share = std::max({keys / (most - 0.5 * tiles), (double)longest / PAGED_MAX_SPLITS, 128.0});
-    auto whole = [](double s) { return ((int)std::ceil(s) + 63) / 64 * 64; };      // (tiles of 64 keys, steps of 32)
-    while (share < longest && items(whole(share)) > most) share *= 1.0625;
-    if (share >= longest) return 0;
-    const int parts = (longest - 1) / whole(share) + 1, even = whole((longest - 1) / parts + 1);
-    return items(even) <= most ? even : whole(share);
+    const int keys = element_bytes == 2 ? 32 : 16, held = d == 64 ? 4 : element_bytes == 2 ? 3 : 2;
+    const double pipe = element_bytes == 2 ? 2.5 * d + 80 : 6.8 * d, bytes = 8.0 * keys * d * element_bytes;
+    return {keys, held, {std::max({700.0, pipe, bytes / (far ? 28 : 45)}), std::max({700.0, 2 * pipe, 2 * bytes / (far ? 43 : 70)})}};
+}
+constexpr int PAGED_JOIN_PARTS = 40;                 // that a row's last one joins; of more a kernel of its own does
+
+// Entities of a launch: tiles (of all key heads) over a sequence each.
+struct PagedTiles {
+    int n = 0;
+    int tiles[PAGED_BATCH + PAGED_POOLS], len[PAGED_BATCH + PAGED_POOLS];
+    void add(int rows, int kv, int length)
+    {
+        tiles[n] = (rows + 15) / 16 * kv;
+        len[n++] = length;
+    }
+};
+inline PagedTiles paged_tiles(const PagedArgs& a, PagedPools pools)
+{
+    PagedTiles t;
+    for (int i = 0; i < a.n; ++i) {
+        const int g = prefix_of(a.req[i]);
+        t.add(a.row[i + 1] - a.row[i], a.n_kv_heads, own_len_of(a.req[i]) + (pools == PagedPools::NONE && g >= 0 ? up16(a.pool[g].len) : 0));
+    }
+    if (pools == PagedPools::TILES)
+        for (int g = 0; g < a.n_pools; ++g) t.add(a.row[a.pool[g].end] - a.row[a.pool[g].begin], a.n_kv_heads, a.pool[g].len);
+    return t;
 }
 
-// Requests of few rows, gathered: tiles and parts.  n_cu: compute units; pools: whether prefixes' tiles are of 16 rows, too, in the same launch.
-inline void plan_paged_few(PagedArgs& a, int element_bytes, int n_cu, bool pools)
+// The cheapest cut with prefixes so.  `unique`: bytes that have to come from memory at least.
+inline PagedCut paged_cut(const PagedArgs& a, PagedPools pools, int element_bytes, int n_cu, double unique, int room)
 {
     const int d = paged_width(a.head_dim);
-    auto tiles_of = [](int rows) { return (long long)(rows + 15) / 16; };
-    auto rows_of = [&](int i) { return a.row[i + 1] - a.row[i]; };
+    const PagedCosts c = paged_costs(d, element_bytes, unique > 128e6);
+    const PagedTiles t = paged_tiles(a, pools);
+    PagedCut best{pools, 0, 1e30};
     int longest = 0;
-    long long tiles = 0;
     double keys = 0;
-    auto more = [&](long long n, int len) {
-        tiles += n * a.n_kv_heads;
-        keys += (double)n * a.n_kv_heads * len;
-        longest = std::max(longest, len);
-    };
-    for (int i = 0; i < a.n; ++i) more(tiles_of(rows_of(i)), paged_len(a, i));
-    if (pools)
-        for (int g = 0; g < a.n_pools; ++g) more(tiles_of(a.row[a.pool[g].end] - a.row[a.pool[g].begin]), a.pool[g].len);
-    auto cut = [&](int share) {
+    for (int i = 0; i < t.n; ++i) {
+        longest = std::max(longest, t.len[i]);
+        keys += (double)t.tiles[i] * t.len[i];
+    }
+    int whole = 64;
+    while (whole < longest) whole *= 2;
+    for (int log = log2_of(whole); log >= 6; --log) {
         long long items = 0;
-        for (int i = 0; i < a.n; ++i) {
-            a.req[i].first = (int)items;
-            items += tiles_of(rows_of(i)) * a.n_kv_heads * paged_parts(paged_len(a, i), share);
+        for (int i = 0; i < t.n; ++i) items += (long long)t.tiles[i] * std::max(1, (t.len[i] + (1 << log) - 1) >> log);
+        const int parts = std::max(1, (longest + (1 << log) - 1) >> log);
+        const bool eight = items <= n_cu;
+        if ((parts > 1 || pools != PagedPools::NONE) && items > room) break;
+        if (parts > PAGED_MAX_SPLITS) break;
+        const double at_once = (double)n_cu * (eight ? 1 : c.held), per = (eight ? 8 : 4) * c.keys, step = c.step[eight];
+        // what bounds it, of which none hides another altogether: the longest part; all of them, one behind the other; memory's rate and the L2s'
+        const double bounds[4] = {PAGED_START + std::ceil(std::min(longest, 1 << log) / per) * step, items > at_once ? (items * (PAGED_START + 0.5 * step) + keys / per * step) / at_once : 0,
+                                  unique / 4800 + 2500, 2.0 * keys * a.head_dim * element_bytes / 9000 + 2500};
+        double ns = 0;
+        for (double x : bounds) ns += x * x * x;
+        ns = std::cbrt(ns);
+        const int meet = parts + (pools == PagedPools::TILES);
+        if (meet > 1) ns += meet <= PAGED_JOIN_PARTS ? 2500 + 100 * meet : 6000;
+        if (ns < best.ns) best = PagedCut{pools, parts > 1 ? 1 << log : 0, ns};
+        if (items > 2 * at_once && parts > 1) break;
+    }
+    if (best.share) {                    // the longest sequence's parts of one length, where that makes no more of them for others
+        const int parts = (longest - 1) / best.share + 1, even = ((longest + parts - 1) / parts + 31) / 32 * 32;
+        long long items = 0, evenly = 0;
+        for (int i = 0; i < t.n; ++i) {
+            items += (long long)t.tiles[i] * paged_parts(t.len[i], best.share);
+            evenly += (long long)t.tiles[i] * paged_parts(t.len[i], even);
         }
-        a.pool_first = (int)items;
-        if (pools)
-            for (int g = 0; g < a.n_pools; ++g) {
-                a.pool[g].first = (int)items;
-                items += tiles_of(a.row[a.pool[g].end] - a.row[a.pool[g].begin]) * a.n_kv_heads * paged_parts(a.pool[g].len, share);
-            }
-        return items;
-    };
-    // Whether parts pay: what a compute unit has to bring of whole sequences goes by latency, parts come at memory's rate but have to be joined (measured for cross attention; where prefixes are
-    // read apart there is something to join anyhow).
-    const double row = 2.0 * a.head_dim * element_bytes, all = keys * row, rate = all <= 256 << 20 ? 45e3 : d == 64 ? 22e3 : 32e3;
-    const double here = (longest + (double)((tiles - 1) / n_cu) * keys / tiles) * row;
-    const bool alike = longest * (double)tiles <= 1.25 * keys;
-    const int most = (d == 128 ? 2 : alike ? 4 : 8) * n_cu;
-    a.share = 0;
-    if ((pools && a.n_pools) || here / rate > 1.1 * all / 5.1e6 + 5) a.share = paged_share(keys, tiles, longest, most, cut);
-    a.pool_share = a.share;
+        if (evenly <= items) best.share = even;
+    }
+    return best;
+}
+
+// Numbers of a launch's tiles; pools: of prefixes of their own in it.
+inline void plan_paged_few(PagedArgs& a, const PagedCut& cut)
+{
+    a.pooled = cut.pools != PagedPools::NONE && a.n_pools;
+    a.share = a.pool_share = cut.share;
     a.pool_height = PAGED_FEW_ROWS;
-    a.items = (int)cut(a.share);
-    a.pool_parts = a.parts + (size_t)a.pool_first * paged_part_floats(16, d);
+    const bool pools = a.pooled && cut.pools == PagedPools::TILES;
+    long long items = 0;
+    int most = 1;
+    a.per = 0;
+    for (int i = 0; i < a.n; ++i) {
+        a.req[i].first = (int)items;
+        const int parts = paged_parts(paged_len(a, a.req[i]), cut.share), mine = (a.row[i + 1] - a.row[i] + 15) / 16 * a.n_kv_heads * parts;
+        a.per = i == 0 || a.per == mine ? mine : 0;
+        most = std::max(most, parts);
+        items += mine;
+    }
+    a.pool_first = (int)items;
+    if (pools)
+        for (int g = 0; g < a.n_pools; ++g) {
+            const int parts = paged_parts(a.pool[g].len, cut.share);
+            a.pool[g].first = (int)items;
+            most = std::max(most, parts + 1);
+            items += (long long)((a.row[a.pool[g].end] - a.row[a.pool[g].begin] + 15) / 16) * a.n_kv_heads * parts;
+        }
+    a.items = (int)items;
+    if (a.per > 4096) a.per = 0;         // (128 requests' tiles times those of one: less than 2^32)
+    a.by_per = by_of(a.per);
+    a.join = (pools || (!a.pooled && most > 1)) && most <= PAGED_JOIN_PARTS;
+    a.subs = most <= 4 ? 1 : 4;
+    a.pool_parts = a.parts + (size_t)a.pool_first * paged_part_floats(16, paged_width(a.head_dim));
 }
 
 // Shares of the XCDs: tiles in runs of equal work.  `entry(i, tiles, each)` gives the i-th entry's tiles and one's work.
@@ -95,20 +161,37 @@ template <typename Entry> int plan_runs(PagedArgs& a, int first, int n, Entry en
     return at;
 }
 
+// The split of a launch's sequences into parts of one length: shortest that `most` workgroups go through at once.  0: none.
+template <typename Items> int paged_share(double keys, long long tiles, int longest, int most, Items items)
+{
+    if (2 * tiles > most) return 0;
+    double share = std::max({keys / (most - 0.5 * tiles), (double)longest / PAGED_MAX_SPLITS, 128.0});
+    auto whole = [](double s) { return ((int)std::ceil(s) + 63) / 64 * 64; };      // (tiles of 64 keys, steps of 32)
+    while (share < longest && items(whole(share)) > most) share *= 1.0625;
+    if (share >= longest) return 0;
+    const int parts = (longest - 1) / whole(share) + 1, even = whole((longest - 1) / parts + 1);
+    return items(even) <= most ? even : whole(share);
+}
+
 // Prefixes' tiles of many rows, in a launch of their own behind that of the requests' own rows.
 inline int pool_rows(const PagedArgs& a, int g) { return a.row[a.pool[g].end] - a.row[a.pool[g].begin]; }
-// Their height, 0: tiles of 16 serve (few rows of each, short ones, or no room for the parts).
+// Their height, 0: no room for the parts.
 inline int paged_pool_height(const PagedArgs& a, int n_cu)
 {
     int most = 0;
-    for (int g = 0; g < a.n_pools; ++g)
-        if (a.pool[g].len >= 512) most = std::max(most, pool_rows(a, g));
-    if (most < 64) return 0;
+    for (int g = 0; g < a.n_pools; ++g) most = std::max(most, pool_rows(a, g));
     const int height = most > 64 ? 128 : 64;
     long long tiles = 0, own = 0;
     for (int g = 0; g < a.n_pools; ++g) tiles += (pool_rows(a, g) + height - 1) / height * a.n_kv_heads;
     for (int i = 0; i < a.n; ++i) own += (a.row[i + 1] - a.row[i] + 15) / 16 * a.n_kv_heads;
     return tiles * height <= (paged_room(a.n_kv_heads) - std::max<long long>(own, 8 * n_cu)) * PAGED_FEW_ROWS ? height : 0;
+}
+// What they should take, with the kernel that joins their rows (us: a tile's 64 keys 1.9 with a workgroup a compute unit, 3 with two).
+inline double paged_pools_ns(const PagedArgs& a, int height, int n_cu)
+{
+    double work = 0;
+    for (int g = 0; g < a.n_pools; ++g) work += (double)((pool_rows(a, g) + height - 1) / height) * a.n_kv_heads * (a.pool[g].len / 64 + 1) * 1500;
+    return 9000 + work / n_cu + 5000 + (double)a.rows * a.n_kv_heads * 10 * 520 / 3500;
 }
 inline void plan_paged_pools(PagedArgs& a, int height, int n_cu)
 {
@@ -146,7 +229,7 @@ inline int plan_paged_many(PagedArgs& a, int n_cu)
     int longest = 0;
     for (int i = 0; i < a.n; ++i) {
         large += (long long)(a.row[i + 1] - a.row[i] + 255) / 256 * a.n_kv_heads;
-        longest = std::max(longest, paged_len(a, i));
+        longest = std::max(longest, paged_len(a, a.req[i]));
     }
     const int height = longest >= 1024 && large >= n_cu - n_cu / 4 ? 256 : 128;
     auto tiles_of = [&](int i) { return (a.row[i + 1] - a.row[i] + height - 1) / height * a.n_kv_heads; };
@@ -155,12 +238,13 @@ inline int plan_paged_many(PagedArgs& a, int n_cu)
         a.req[i].first = at;
         at += tiles_of(i);
     }
-    a.share = a.pool_share = 0;
+    a.share = a.pool_share = a.per = 0;
+    a.join = false;
     a.pool_height = height;
     a.items = a.pool_first = at;
     plan_runs(a, 0, a.n, [&](int i) {
         const int q = (a.row[i + 1] - a.row[i]) / (a.n_heads / a.n_kv_heads);
-        return std::pair<int, double>(tiles_of(i), OWN + paged_len(a, i) - (a.causal ? std::min(q, a.req[i].own_len) / 2 : 0));
+        return std::pair<int, double>(tiles_of(i), OWN + paged_len(a, a.req[i]) - (a.causal ? std::min(q, own_len_of(a.req[i])) / 2 : 0));
     });
     return height;
 }

@@ -60,6 +60,5 @@ inline int check_rows(const char* name, const void* at, long long width, long lo
 }
 
 inline bool is_page_rows(int n, int least, int most) { return n >= least && n <= most && (n & (n - 1)) == 0; }
-inline int log2_of(int n) { return 31 - __builtin_clz((unsigned)n); }
 
 }  // namespace tts

@@ -68,9 +68,12 @@ hipError_t launch_append(AppendArgs& a, bool x_bf16, bool bf16, int n_cu, hipStr
 // Requests of one prefix lie side by side.  A sequence of keys is a prefix's rows and a request's own behind them, which begin at a whole 16 (the keys between do not exist).
 constexpr int PAGED_BATCH = 128, PAGED_SMALL = 16, PAGED_POOLS = 32;     // requests of a launch, prefixes
 struct PagedReq {
-    int own_len, table_row, q_row;
+    unsigned len_prefix;                 // rows of its own, and above 25 bits of them 1 + its prefix, 0: none
+    int table_row, q_row;
     int first;                           // of its tiles (of all key heads and parts), in the launch
 };
+__host__ __device__ inline int own_len_of(const PagedReq& r) { return (int)(r.len_prefix & 0x1FFFFFFu); }
+__host__ __device__ inline int prefix_of(const PagedReq& r) { return (int)(r.len_prefix >> 25) - 1; }
 struct PagedPool {
     int table_row, len;
     int begin, end;                      // its requests in the launch
@@ -81,39 +84,54 @@ struct PagedCommon {
     const int* table;
     void* out;
     float *lse, *parts, *pool_parts;     // parts of requests' tiles; of prefixes'
+    int part_floats;                     // room for parts, in floats
+    int* arrived;                        // how many of a row's parts are there: [key heads][rows], zeros between launches
     long long q_stride, out_stride, page_stride;               // elements
     float scale;                         // times log2(e)
     int n_heads, n_kv_heads, head_dim, n_pages, table_cols, page_shift;
-    int n, n_pools;
+    int n, n_pools, rows;                // rows of all requests (of one key head)
     int each;                            // rows of every request, 0: they differ
+    int per;                             // tiles of every request, 0: they differ
+    unsigned by_per, by_group;           // 2^32 / per, 2^32 / group, rounded up (group: of query heads to a key head), for over(); by_group NOT_BY where that is not exact
+    int q_first;                         // query row of the launch's first query, where they lie back to back; -1: they do not
     int items;                           // tiles of the launch
     int share, pool_share;               // length of a part of a request's keys, of a prefix's, 0: they have none
     int pool_first, pool_height;         // first tile that is a prefix's; rows of such a tile
     bool causal;
     bool pooled;                         // prefixes have tiles of their own, over all their requests' rows; otherwise a request's keys begin with its prefix's
+    bool join;                           // a row's last part to arrive joins them, in so many sums
+    int subs;
     int start[9];                        // many rows: first of the tiles that each XCD takes
 };
+// x / y by 2^32 / y rounded up; y = 1: by 0.  Exact while x * y <= 2^32, for powers of two always.
+constexpr unsigned by_of(unsigned y) { return y <= 1 ? 0 : (unsigned)(((1ull << 32) + y - 1) / y); }
+constexpr unsigned NOT_BY = ~0u;         // (of no y)
+__host__ __device__ inline int over(int x, unsigned by)
+{
+    return by ? (int)(((unsigned long long)(unsigned)x * by) >> 32) : x;
+}
 template <int N> struct PagedArgsOf : PagedCommon {
     static constexpr int BATCH = N, POOLS = N < PAGED_POOLS ? N : PAGED_POOLS;
     PagedReq req[N];
     PagedPool pool[POOLS];
     int row[N + 1];
-    signed char pool_of[N];              // -1: none
 };
 using PagedArgs = PagedArgsOf<PAGED_BATCH>;
-constexpr int up16(int n) { return (n + 15) / 16 * 16; }
 // Length of a request's keys, with its prefix's if that is not read apart; parts of a length (one without keys, too, where there are none)
-template <typename Args> __host__ __device__ inline int paged_len(const Args& a, int i)
+template <typename Args> __host__ __device__ inline int paged_len(const Args& a, const PagedReq& r)
 {
-    return a.req[i].own_len + (a.pooled || a.pool_of[i] < 0 ? 0 : (a.pool[(int)a.pool_of[i]].len + 15) / 16 * 16);
+    const int g = prefix_of(r);
+    return own_len_of(r) + (a.pooled || g < 0 ? 0 : (a.pool[g].len + 15) / 16 * 16);
 }
 __host__ __device__ inline int paged_parts(int len, int share) { return share == 0 || len <= share ? 1 : (len - 1) / share + 1; }
+inline int log2_of(int n) { return 31 - __builtin_clz((unsigned)n); }
+constexpr int up16(int n) { return (n + 15) / 16 * 16; }
 constexpr int PAGED_FEW_ROWS = 16;       // of a tile
 constexpr size_t paged_part_floats(int rows, int d) { return (size_t)rows * (d + 2); }
 constexpr int paged_width(int head_dim) { return head_dim > 64 ? 128 : 64; }
 hipError_t allow_paged();                // once on each device, before the first launch there
-hipError_t launch_paged_few(const PagedArgs& a, bool bf16, hipStream_t s);      // tiles of 16 rows
+hipError_t launch_paged_few(const PagedArgs& a, bool bf16, int n_cu, hipStream_t s);     // tiles of 16 rows
 hipError_t launch_paged_many(const PagedArgs& a, int height, hipStream_t s);    // of 64, 128 or 256, two bytes
-hipError_t launch_paged_join(const PagedArgs& a, bool bf16, hipStream_t s);     // rows of requests that have a prefix apart or parts
+hipError_t launch_paged_join(const PagedArgs& a, bool bf16, hipStream_t s);     // rows of requests that have a prefix apart or parts, where their last part does not join them
 
 }  // namespace tts

@@ -23,7 +23,7 @@ void look_at(const tts::PagedArgs& a, int height, bool requests, bool prefixes)
     bool apart = false;
     expect(a.n >= 1 && a.n <= PAGED_BATCH && a.n_pools <= PAGED_POOLS && a.row[0] == 0, "numbers of the launch");
     for (int i = 0; requests && i < a.n; ++i) {
-        const int rows = a.row[i + 1] - a.row[i], len = paged_len(a, i), parts = paged_parts(len, a.share), g = a.pool_of[i];
+        const int rows = a.row[i + 1] - a.row[i], len = paged_len(a, a.req[i]), parts = paged_parts(len, a.share), g = prefix_of(a.req[i]);
         expect(rows > 0 && rows % group == 0 && (!a.each || rows == a.each), "rows of a request");
         expect(g < a.n_pools && (g < 0 || (a.pool[g].begin <= i && i < a.pool[g].end)), "a request's prefix");
         expect(a.req[i].first == at, "a request's first tile");
@@ -48,7 +48,10 @@ void look_at(const tts::PagedArgs& a, int height, bool requests, bool prefixes)
     expect(!prefixes || (a.pool_parts - a.parts >= a.pool_first * (long long)paged_part_floats(16, paged_width(a.head_dim)) && a.pool_parts - a.parts + pool_floats <= room), "room for prefixes' parts");
     expect(a.items == at, "tiles of the launch");
     pools += prefixes ? a.n_pools : 0;
-    parts_pending |= apart || prefixes;
+    expect(!a.join || ((apart || prefixes) && (prefixes || !a.pooled || !a.n_pools) && (long long)a.rows * a.n_kv_heads <= 16LL * paged_room(a.n_kv_heads)), "parts that the last one joins");
+    expect(a.rows == a.row[a.n] && (!requests || a.per == 0 || a.per * a.n == a.pool_first), "numbers of the launch");
+    parts_pending |= (apart || prefixes) && !a.join;
+    joins += a.join;
     pools_pending = requests && !prefixes && a.pooled && a.n_pools;
 }
 tts::RotaryArgs rotary;
@@ -74,7 +77,7 @@ hipError_t launch_append(AppendArgs& a, bool, bool, int, hipStream_t)
     return call("launch");
 }
 hipError_t allow_paged() { return call("allow"); }
-hipError_t launch_paged_few(const PagedArgs& a, bool, hipStream_t)
+hipError_t launch_paged_few(const PagedArgs& a, bool, int, hipStream_t)
 {
     ++launches;
     ++few;

@@ -216,12 +216,10 @@ def test_paged_refuses(lib):
     def run(**change):
         return _paged(lib, m, **change)
 
-    assert run() == 0 and lib.fake_requests_seen() == 2 and lib.past_rows() == 20 and lib.past_pools() == 2 and lib.past_joins() == 1          # a request without queries is left out
-    lib.past_reset()
-    assert run(prefix=None) == 0 and lib.past_pools() == 0 and lib.past_joins() == 0
-    assert run(prefix=(-1, 0, -1)) == 0 and lib.past_pools() == 0                                                                               # nobody's prefix is not read
+    assert run() == 0 and lib.fake_requests_seen() == 2 and lib.past_rows() == 20                # a request without queries is left out
+    assert run(prefix=None) == 0 and run(prefix=(-1, 0, -1)) == 0
     assert run(q_len=(0, 0, 0), q=None, out=None, k_pages=None, v_pages=None, table=None) == 0
-    assert run(own=(0, 0, 0), table_row=(9, -1, 5), lens=(0, 0), rows=(-1, 99), k_pages=None, v_pages=None, table=None) == 0 and lib.past_pools() == 0
+    assert run(own=(0, 0, 0), table_row=(9, -1, 5), lens=(0, 0), rows=(-1, 99), k_pages=None, v_pages=None, table=None) == 0
     assert run(prefix=None, lens=(), rows=()) == 0 and run(lse=None) == 0 and run(own=(128, 1, 97)) == 0 and run(scale=0.5) == 0
     assert run(page_stride=2 * 32 * 40 + 8, q_stride=328, out_stride=1 << 40) == 0
     for change in (dict(n=0), dict(n=-1), dict(null="q_len"), dict(null="own_len"), dict(null="table_row"), dict(null="prefix_len"), dict(null="prefix_table_row"), dict(q_len=(-1, 0, 0)),
@@ -263,6 +261,23 @@ def test_plans_of_attention(lib, heads, kv, d, bf16):
                     lib.past_reset()
                     assert _paged(lib, m, q_len, own, [0] * n, prefix, lens, [1] * prefixes, table_cols=2000) == 0
                     assert lib.fake_requests_seen() == sum(q > 0 for q in q_len) and lib.past_rows() == sum(q_len) * (heads // kv), (n, q_hi, own_hi, prefixes)
+    m.close()
+
+
+@pytest.mark.parametrize("shape,q_len,own,prefix,lens,want", [
+    ((8, 8, 64), [1] * 64, 300, [0] * 64, [2000], dict(few=1, many=0, pools=1, joins=1)),                # a prefix in tiles of its own beside the requests', joined by their last parts
+    ((32, 8, 128), [1] * 128, 200, [0] * 128, [16001], dict(few=1, many=1, pools=1, joins=1)),           # larger tiles, a launch for them and one that joins
+    ((8, 8, 64), [1, 2], 30, [0, 0], [41], dict(few=1, many=0, pools=0, joins=0)),                       # a short one ahead of each request's own rows
+    ((8, 8, 64), [1] * 64, 300, [-1] * 64, [2000], dict(few=1, many=0, pools=0, joins=0)),               # nobody's prefix is not read
+    ((4, 4, 64), [1], 9000, [-1], [], dict(few=1, many=0, pools=0, joins=1)),                            # a long sequence in parts
+    ((16, 4, 128), [2000] * 8, 2000, [0] * 8, [500], dict(few=0, many=1, pools=0, joins=0)),             # many rows
+])
+def test_how_calls_are_taken(lib, shape, q_len, own, prefix, lens, want):
+    lib.past_reset()
+    m = Made(lib, "paged", binding.make_paged_config(*shape, 16, True))
+    n = len(q_len)
+    assert _paged(lib, m, q_len, [own] * n, [0] * n, prefix, lens, [1] * len(lens), table_cols=2000) == 0
+    assert {k: getattr(lib, f"past_{k}")() for k in want} == want
     m.close()
 
 
