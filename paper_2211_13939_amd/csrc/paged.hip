@@ -104,6 +104,11 @@ struct Item {
     int request, request_row, queries;   // of one request: which, its first row, its queries; -1: a prefix's
     int pool;                            // its prefix, read apart, -1: none
     int slots;                           // 1, 2, 4, 8 or 16: rows of the tile at most
+    // how many keys a row may see
+    template <typename Args> __device__ __forceinline__ int limit_of(const Args& p, int row) const
+    {
+        return p.causal && request >= 0 ? seq.own_at + max(0, seq.own_len - queries + rows_to_queries(p, row - request_row) + 1) : NO_LIMIT;
+    }
 };
 template <int HEIGHT, typename Args> __device__ __forceinline__ Item item_of(const Args& p, Requests<Args>& all, int id)
 {
@@ -206,19 +211,21 @@ struct Row {
     long long q_row;
     int head, limit;
     int request;                         // of rows of a prefix that asked for it
+    __device__ __forceinline__ Row() {}
+    template <typename Args> __device__ __forceinline__ void of_request(const Args& p, const Item& t, int row)
+    {
+        const int group = p.n_heads / p.n_kv_heads, in = row - t.request_row, query = rows_to_queries(p, in);
+        q_row = (long long)(p.q_first >= 0 ? p.q_first + rows_to_queries(p, t.request_row) : p.req[t.request].q_row) + query;
+        head = t.kv * group + in - query * group;
+    }
     template <typename Args> __device__ __forceinline__ Row(const Args& p, const Requests<Args>& all, const Item& t, int row)
     {
         row = min(row, t.row_end - 1);
         const int group = p.n_heads / p.n_kv_heads;
-        limit = NO_LIMIT;
+        limit = t.limit_of(p, row);
         request = t.request;
-        if (t.request >= 0) {
-            const int in = row - t.request_row, query = rows_to_queries(p, in);
-            // (of a request, which the wave has)
-            q_row = (long long)(p.q_first >= 0 ? p.q_first + rows_to_queries(p, t.request_row) : p.req[t.request].q_row) + query;
-            head = t.kv * group + in - query * group;
-            if (p.causal) limit = t.seq.own_at + max(0, t.seq.own_len - t.queries + query + 1);
-        } else {
+        if (t.request >= 0) of_request(p, t, row);
+        else {
             request = p.each ? row / p.each : all.of_row(p, row);
             const int query = rows_to_queries(p, row);   // (rows of a request: a multiple of the group's heads)
             if (p.q_first >= 0) q_row = (long long)p.q_first + query;
@@ -623,7 +630,7 @@ __device__ __forceinline__ void to_lds_from(const char* base, uint32_t offset, u
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" : "={m0}"(m0) : "s"(to), "v"(offset), "s"(base) : "memory");
 }
 
-template <int D, int NW, int R> __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : NW == 8 ? 4 : 3) void k_paged_many(PagedArgs p)
+template <int D, int NW, int R, bool FULL, typename Args> __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : NW == 8 ? 4 : 3) void k_paged_many(Args p)
 {
     using M = PagedMany<D, NW, R>;
     constexpr int ROW = M::ROW, NK = D / 16, HEIGHT = 32 * NW;
@@ -634,23 +641,36 @@ template <int D, int NW, int R> __global__ __launch_bounds__(64 * NW, D == 128 ?
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
     const int xcd = blockIdx.x & 7, id = p.start[xcd] + (blockIdx.x >> 3);
     if (id >= p.start[xcd + 1]) return;
-    Requests<PagedArgs> all;
+    Requests<Args> all;
     const Item t = item_of<HEIGHT>(p, all, id);
-    const int row = t.first_row + 32 * wave + c;
-    const Row mine(p, all, t, row);
-    ManyRunning<D> run;
-#pragma unroll
-    for (int k = 0; k < NK; ++k) {
-        const int d = 16 * k + 8 * h;
-        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(p.q) + mine.q_row * p.q_stride + mine.head * p.head_dim + (d < p.head_dim ? d : 0));
-        run.q[k] = d < p.head_dim ? x : make_uint4(0, 0, 0, 0);
-    }
-    // keys that the workgroup's last row sees, that the wave's last does, that all of the wave's rows do, and all of the workgroup's
-    const Row last(p, all, t, t.row_end - 1 < t.first_row + HEIGHT - 1 ? t.row_end - 1 : t.first_row + HEIGHT - 1);
-    const int end = min(t.end, __builtin_amdgcn_readfirstlane(last.limit)), wave_end = min(end, __builtin_amdgcn_readlane(mine.limit, 31)), clear = min(end, __builtin_amdgcn_readfirstlane(mine.limit));
-    const Row top(p, all, t, t.first_row);
-    const int all_clear = min(end, __builtin_amdgcn_readfirstlane(top.limit));
+    // keys that the workgroup's last row sees, that all of its rows do; that the wave's last does, that all of the wave's do
+    const int end = min(t.end, t.limit_of(p, min(t.row_end, t.first_row + HEIGHT) - 1)), all_clear = min(end, t.limit_of(p, t.first_row));
+    const int wave_end = min(end, t.limit_of(p, min(t.row_end - 1, t.first_row + 32 * wave + 31))), clear = min(end, t.limit_of(p, min(t.row_end - 1, t.first_row + 32 * wave)));
     const int first_tile = t.begin / KEYS, n_tiles = (end + KEYS - 1) / KEYS;
+    auto look = [&](int first) {         // 64 tiles from `first` on
+        for (int i = threadIdx.x; i < M::AHEAD * KEYS / 16; i += 64 * NW) {
+            const int key = first * KEYS + 16 * i;
+            if (key - 16 * i % KEYS >= end) break;       // (whole tiles)
+            long long at = 0;
+            const int n = key < end ? t.seq.look(p, key, at) : 0;
+            where[(first * (KEYS / 16) + i) % M::SIXTEENS] = 2 * at;
+            which[(first * (KEYS / 16) + i) % M::SIXTEENS] = (uint16_t)((1u << n) - 1);
+        }
+    };
+    look(first_tile);
+    const int row = t.first_row + 32 * wave + c;
+    const int limit = t.limit_of(p, min(row, t.row_end - 1));
+    ManyRunning<D> run;
+    {
+        const Row mine(p, all, t, row);
+        const bf16_t* from = static_cast<const bf16_t*>(p.q) + mine.q_row * p.q_stride + mine.head * p.head_dim;
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+            const int d = 16 * k + 8 * h;
+            const uint4 x = *reinterpret_cast<const uint4*>(from + (FULL || d < p.head_dim ? d : 0));
+            run.q[k] = FULL || d < p.head_dim ? x : make_uint4(0, 0, 0, 0);
+        }
+    }
     // this wave's share of a tile: the row and piece that lie where the lane's 16 bytes go
     int from_row[M::LOADS];
     uint32_t k_offset[M::LOADS], v_offset[M::LOADS];
@@ -659,43 +679,44 @@ template <int D, int NW, int R> __global__ __launch_bounds__(64 * NW, D == 128 ?
     for (int i = 0; i < M::LOADS; ++i) {
         const int at = (wave + i * NW) * 1024 + lane * 16, at_row = at / ROW, piece = at % ROW / 16, k_piece = key_piece<D>(at_row, piece), v_piece = value_piece<D>(at_row, piece);
         from_row[i] = at_row;
-        k_there[i] = 8 * k_piece < p.head_dim;
-        v_there[i] = 8 * v_piece < p.head_dim;
+        k_there[i] = FULL || 8 * k_piece < p.head_dim;
+        v_there[i] = FULL || 8 * v_piece < p.head_dim;
         k_offset[i] = 2 * (at_row % 16 * p.head_dim + 8 * k_piece);
         v_offset[i] = 2 * (at_row % 16 * p.head_dim + 8 * v_piece);
     }
     const uint32_t lds_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds;
     const size_t head_at = (size_t)t.kv * (p.head_dim << p.page_shift) * 2;
     const char *kp = static_cast<const char*>(p.k_pages) + head_at, *vp = static_cast<const char*>(p.v_pages) + head_at;
-    auto look = [&](int first) {         // 64 tiles from `first` on
-        for (int i = threadIdx.x; i < M::AHEAD * KEYS / 16; i += 64 * NW) {
-            const int key = first * KEYS + 16 * i;
-            long long at;
-            const int n = key < end ? t.seq.look(p, key, at) : 0;
-            where[(first * (KEYS / 16) + i) % M::SIXTEENS] = n ? 2 * at : 0;
-            which[(first * (KEYS / 16) + i) % M::SIXTEENS] = (uint16_t)((1u << n) - 1);
-        }
-    };
     auto same = [](uint64_t x) -> uint64_t {             // of a value that all lanes have
         const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)x), high = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
         return (uint64_t)high << 32 | low;
     };
-    auto there = [&](int tile) { return same(*reinterpret_cast<const uint64_t*>(which + tile * (KEYS / 16) % M::SIXTEENS)); };
-    auto bring = [&](int tile, int slot) {
+    // where a tile's keys lie that this wave brings (asked for ahead: a trip to LDS for each would stand in every tile's way)
+    struct Froms { uint64_t at[M::LOADS]; };
+    auto ask = [&](int tile) {
+        Froms f;
+#pragma unroll
+        for (int i = 0; i < M::LOADS; ++i) f.at[i] = (uint64_t)where[(tile * (KEYS / 16) + (wave + i * NW) * 1024 / ROW / 16) % M::SIXTEENS];
+        return f;
+    };
+    auto ask_which = [&](int tile) { return *reinterpret_cast<const uint64_t*>(which + tile * (KEYS / 16) % M::SIXTEENS); };
+    auto bring = [&](const Froms& f, int slot) {
+        uint64_t from[M::LOADS];
+#pragma unroll
+        for (int i = 0; i < M::LOADS; ++i) from[i] = same(f.at[i]);
 #pragma unroll
         for (int i = 0; i < M::LOADS; ++i) {
-            const long long from = (long long)same((uint64_t)where[(tile * (KEYS / 16) + (wave + i * NW) * 1024 / ROW / 16) % M::SIXTEENS]);
             const uint32_t to = lds_at + slot * M::SLOT + (wave + i * NW) * 1024;
-            if (k_there[i]) to_lds_from(kp + from, k_offset[i], to);
-            if (v_there[i]) to_lds_from(vp + from, v_offset[i], to + M::PART);
+            if (k_there[i]) to_lds_from(kp + from[i], k_offset[i], to);
+            if (v_there[i]) to_lds_from(vp + from[i], v_offset[i], to + M::PART);
         }
     };
-    if (p.head_dim < D)                  // (columns that there are not: zeros, which nothing is loaded over)
+    if (!FULL)                           // (columns that there are not: zeros, which nothing is loaded over)
         for (int i = threadIdx.x; i < R * M::SLOT / 16; i += 64 * NW) reinterpret_cast<uint4*>(lds)[i] = make_uint4(0, 0, 0, 0);
-    look(first_tile);
     if (threadIdx.x == 0) *odd = 0;
     __syncthreads();
-    for (int i = 0; i < R - 1 && first_tile + i < n_tiles; ++i) bring(first_tile + i, i);
+    for (int i = 0; i < R - 1 && first_tile + i < n_tiles; ++i) bring(ask(first_tile + i), i);
+    uint64_t next_which = ask_which(first_tile);
     // The queries are here, with the first tile: waited for in the loop, they would be together with the tiles that are on their way.
 #pragma unroll
     for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(run.q[k].x), "+v"(run.q[k].y), "+v"(run.q[k].z), "+v"(run.q[k].w));
@@ -707,12 +728,13 @@ template <int D, int NW, int R> __global__ __launch_bounds__(64 * NW, D == 128 ?
             look(tile + M::AHEAD / 2);
             __syncthreads();
         }
-        if (tile + R - 1 < n_tiles) bring(tile + R - 1, free);
-        const uint64_t mask = there(tile);
+        if (tile + R - 1 < n_tiles) bring(ask(tile + R - 1), free);
+        const uint64_t mask = same(next_which);
+        next_which = ask_which(tile + 1);
         const char* keys = lds + slot * M::SLOT;
         char* values = lds + slot * M::SLOT + M::PART;
         const int key = tile * KEYS;
-        if (mask != 0 && (mask != ~0ull || key + KEYS > all_clear)) {
+        if (mask != ~0ull || key + KEYS > all_clear) {
             // values of keys that there are not: zeros (0 times an infinity would be NaN); infinities and NaN of those that not all rows see are taken out
             bool bad = false;
 #pragma unroll
@@ -729,11 +751,10 @@ template <int D, int NW, int R> __global__ __launch_bounds__(64 * NW, D == 128 ?
             if (bad) *odd = 1;
             lds_barrier();
         }
-        if (mask != 0 && key < wave_end) {
-            const int seen = min(mine.limit, end) - key;
-            const uint64_t own = key + KEYS <= clear ? mask : mask & (seen >= KEYS ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
-            run.template take<2>(keys, values, mask != ~0ull || key + KEYS > clear, own, p.scale, lane);
-        }
+        // (by all waves, also those whose rows end before: the tile's barrier waits for the others, and a branch here has the compiler copy all sums from turn to turn)
+        const int seen = min(limit, end) - key;
+        const uint64_t own = key + KEYS <= clear ? mask : mask & (seen >= KEYS ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
+        run.template take<2>(keys, values, mask != ~0ull || key + KEYS > clear, own, p.scale, lane);
         free = slot;                                     // (the slot that the tile before this one was in)
         slot = slot + 1 == R ? 0 : slot + 1;
     }
@@ -749,7 +770,7 @@ template <int D, int NW, int R> __global__ __launch_bounds__(64 * NW, D == 128 ?
                 for (int i = 0; i < 16; ++i) {
                     const int column = 32 * d + 8 * (i / 4) + 4 * h + (i & 3);
                     const float x = not_finite(value[min(column, p.head_dim - 1)]);
-                    run.o[d][i] += key < mine.limit ? x : 0.f;
+                    run.o[d][i] += key < limit ? x : 0.f;
                 }
         }
     const float l = run.sum(), m = run.m;
@@ -766,6 +787,11 @@ template <int D, int NW, int R> __global__ __launch_bounds__(64 * NW, D == 128 ?
         }
         return;
     }
+    // (looked up again: its registers are the loop's)
+    int again = min(row, t.row_end - 1);
+    asm volatile("" : "+v"(again));
+    Row mine;
+    mine.of_request(p, t, again);
     run.store(static_cast<bf16_t*>(p.out) + mine.q_row * p.out_stride + mine.head * p.head_dim, l == 0.f ? 0.f : 1.0f / l, row < t.row_end, p.head_dim, lane);
     if (p.lse && row < t.row_end && h == 0) p.lse[mine.q_row * p.n_heads + mine.head] = log_sum(m, l);
 }
@@ -891,12 +917,24 @@ template <int D, int NW, int R> hipError_t go_many(const PagedArgs& a, hipStream
 {
     int most = 0;
     for (int i = 0; i < 8; ++i) most = std::max(most, a.start[i + 1] - a.start[i]);
-    hipLaunchKernelGGL((k_paged_many<D, NW, R>), dim3(8 * most), dim3(64 * NW), (PagedMany<D, NW, R>::LDS), s, a);
-    return hipGetLastError();
+    return with_args(a, [&](const auto& args) {
+        using Args = std::decay_t<decltype(args)>;
+        if (a.head_dim == D) hipLaunchKernelGGL((k_paged_many<D, NW, R, true, Args>), dim3(8 * most), dim3(64 * NW), (PagedMany<D, NW, R>::LDS), s, args);
+        else hipLaunchKernelGGL((k_paged_many<D, NW, R, false, Args>), dim3(8 * most), dim3(64 * NW), (PagedMany<D, NW, R>::LDS), s, args);
+        return hipGetLastError();
+    });
+}
+template <int D, int NW, int R, bool FULL, int BATCH> hipError_t allow_one()
+{
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_paged_many<D, NW, R, FULL, PagedArgsOf<BATCH>>), hipFuncAttributeMaxDynamicSharedMemorySize, PagedMany<D, NW, R>::LDS);
 }
 template <int D, int NW, int R> hipError_t allow()
 {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_paged_many<D, NW, R>), hipFuncAttributeMaxDynamicSharedMemorySize, PagedMany<D, NW, R>::LDS);
+    hipError_t e = allow_one<D, NW, R, true, PAGED_BATCH>();
+    if (e == hipSuccess) e = allow_one<D, NW, R, false, PAGED_BATCH>();
+    if (e == hipSuccess) e = allow_one<D, NW, R, true, PAGED_SMALL>();
+    if (e == hipSuccess) e = allow_one<D, NW, R, false, PAGED_SMALL>();
+    return e;
 }
 
 template <typename T, int D> hipError_t go_join(const PagedArgs& a, hipStream_t s)
