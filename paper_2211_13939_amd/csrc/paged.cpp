@@ -48,7 +48,7 @@ Layout layout_of(const tts_paged_config& c)
     return l;
 }
 
-enum class Form { FEW, WHOLE, MANY };                // tiles of 16 rows, prefixes apart if that pays; tiles of 16 over whole sequences; tiles of 128 or 256
+enum class Form { FEW, WHOLE, MANY };                // tiles of 16 rows, prefixes apart if that pays; tiles of 16 over whole sequences; tiles of 128, or of 16 where that takes less
 
 }  // namespace
 
@@ -142,7 +142,7 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
     a.n_pages = t->n_pages; a.table_cols = t->table_cols; a.page_shift = shift;
     a.causal = c.causal;
     // the requests in the order of their prefixes, those without one first (an empty one is none)
-    const bool bf16 = c.dtype == TTS_DTYPE_BF16, any_many = bf16 && paged_many(few_tiles, p->n_cu);
+    const bool bf16 = c.dtype == TTS_DTYPE_BF16;
     auto prefix_of = [&](int i) { return b->prefix && b->prefix[i] >= 0 && b->prefix_len[b->prefix[i]] > 0 ? b->prefix[i] : -1; };
     int order[TTS_CACHE_MAX_BATCH], q_row[TTS_CACHE_MAX_BATCH], count[TTS_PAGED_MAX_PREFIXES + 2] = {};
     for (int i = 0, at = 0; i < b->n; ++i) {
@@ -153,6 +153,10 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
     for (int g = 0; g <= b->n_prefixes; ++g) count[g + 1] += count[g];
     for (int i = 0; i < b->n; ++i) order[count[prefix_of(i) + 1]++] = i;
     auto rows_of = [&](int i) { return (long long)b->q_len[i] * group; };
+    // small requests beside large ones are a launch with them, if that is a small one
+    bool mixed = false;
+    for (int i = 0; i < b->n; ++i) mixed |= rows_of(i) > 0 && rows_of(i) < PAGED_MANY_ROWS;
+    const bool any_many = bf16 && (!mixed || paged_many(few_tiles, p->n_cu));
     auto form_of = [&](int i) {
         return any_many && rows_of(i) >= PAGED_MANY_ROWS ? Form::MANY : rows_of(i) < PAGED_MANY_ROWS || few_tiles <= 1024 ? Form::FEW : Form::WHOLE;
     };
@@ -181,37 +185,43 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
                 if (a.req[i].q_row != a.req[0].q_row + a.row[i] / group) a.q_first = -1;
             }
             hipError_t e;
-            if (form == Form::MANY) {
-                const int height = plan_paged_many(a, p->n_cu);
-                e = launch_paged_many(a, height, p->stream);
-            } else {
-                // prefixes ahead of each request's own rows, as tiles of their own beside them, or as a launch of larger ones
-                const int bytes = bf16 ? 2 : 4;
-                double unique = 0;
-                for (int i = 0; i < a.n; ++i) unique += own_len_of(a.req[i]);
-                for (int g = 0; g < a.n_pools; ++g) unique += a.pool[g].len;
-                unique *= 2.0 * c.n_kv_heads * c.head_dim * bytes;
-                PagedCut cut = paged_cut(a, PagedPools::NONE, bytes, p->n_cu, unique, room);
-                int height = 0;
-                if (form == Form::FEW && a.n_pools) {
-                    const PagedCut tiles = paged_cut(a, PagedPools::TILES, bytes, p->n_cu, unique, room);
-                    if (tiles.ns < cut.ns) cut = tiles;
-                    height = bf16 ? paged_pool_height(a, p->n_cu) : 0;
-                    if (height) {
-                        PagedCut apart = paged_cut(a, PagedPools::APART, bytes, p->n_cu, unique, 8 * p->n_cu);
-                        apart.ns += paged_pools_ns(a, height, p->n_cu);
-                        if (apart.ns < cut.ns) cut = apart;
-                        else height = 0;
-                    }
+            // what the cheapest way should take: prefixes ahead of each request's own rows, as tiles of their own beside them, or as a launch of larger ones; larger tiles for requests, too
+            const int bytes = bf16 ? 2 : 4;
+            double unique = 0;
+            for (int i = 0; i < a.n; ++i) unique += own_len_of(a.req[i]);
+            for (int g = 0; g < a.n_pools; ++g) unique += a.pool[g].len;
+            unique *= 2.0 * c.n_kv_heads * c.head_dim * bytes;
+            PagedCut cut = paged_cut(a, PagedPools::NONE, bytes, p->n_cu, unique, room);
+            int height = 0;
+            bool many = false;
+            if (form != Form::WHOLE && a.n_pools) {
+                const PagedCut beside = paged_cut(a, PagedPools::TILES, bytes, p->n_cu, unique, room);
+                if (beside.ns < cut.ns) cut = beside;
+                height = bf16 ? paged_pool_height(a, p->n_cu) : 0;
+                if (height) {
+                    PagedCut apart = paged_cut(a, PagedPools::APART, bytes, p->n_cu, unique, 8 * p->n_cu);
+                    apart.ns += paged_pools_ns(a, height, p->n_cu);
+                    if (apart.ns < cut.ns) cut = apart;
+                    else height = 0;
                 }
+            }
+            if (form == Form::MANY) {
+                const PagedCut larger = paged_many_cut(a, p->n_cu, unique);
+                many = larger.ns < cut.ns;
+                if (many) cut = larger;
+            }
+            if (many) {
+                plan_paged_many(a, cut);
+                e = launch_paged_many(a, PAGED_MANY_HEIGHT, p->stream);
+            } else {
                 plan_paged_few(a, cut);
                 e = launch_paged_few(a, bf16, p->n_cu, p->stream);
                 if (e == hipSuccess && height) {
                     plan_paged_pools(a, height, p->n_cu);
                     e = launch_paged_many(a, height, p->stream);
                 }
-                if (e == hipSuccess && !a.join && ((a.pooled && a.n_pools) || a.share)) e = launch_paged_join(a, bf16, p->stream);
             }
+            if (e == hipSuccess && !a.join && ((a.pooled && a.n_pools) || a.share)) e = launch_paged_join(a, bf16, p->stream);
             clear();
             return e;
         };

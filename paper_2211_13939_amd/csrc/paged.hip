@@ -814,7 +814,11 @@ template <typename T, int D, int ACROSS, typename Args> __global__ __launch_boun
         i = __builtin_amdgcn_readfirstlane(all.of_row(p, row));
     }
     const PagedReq r = p.req[i];
-    const int pool = prefix_of(r), own_parts = paged_parts(paged_len(p, r), p.share), in_request = row - p.row[i], own_tiles = (p.row[i + 1] - p.row[i] + 15) / 16;
+    const int pool = prefix_of(r), own_parts = paged_parts(paged_len(p, r), p.share), in_request = row - p.row[i];
+    // (tiles in the order of item_of: of 16 rows a tile's parts one behind the other; of more a part's tiles, the last one first)
+    const bool low = p.height == PAGED_FEW_ROWS;
+    const int own_tiles = (p.row[i + 1] - p.row[i] + p.height - 1) / p.height, own_tile = in_request / p.height, own_step = low ? 1 : own_tiles;
+    const int own_at = r.first + (low ? (kv * own_tiles + own_tile) * own_parts : kv * own_parts * own_tiles + own_tiles - 1 - own_tile);
     int pool_parts = 0, pool_at = 0, pool_step = 0, pool_row = 0;
     if (p.pooled && pool >= 0) {
         const PagedPool o = p.pool[pool];
@@ -827,13 +831,13 @@ template <typename T, int D, int ACROSS, typename Args> __global__ __launch_boun
     }
     const int parts = own_parts + pool_parts;
     const bool todo = in && parts > 1;                   // (whole rows are there already)
-    const float* own = p.parts + (r.first + (kv * own_tiles + in_request / 16) * own_parts) * paged_part_floats(16, D);
+    const float* own = p.parts + own_at * paged_part_floats(p.height, D);
     const float* pre = p.pool_parts + pool_at * paged_part_floats(p.pool_height, D);
     auto part_at = [&](int n, int& height, int& in_tile) -> const float* {
         const bool mine = n < own_parts;
-        height = mine ? 16 : p.pool_height;
-        in_tile = mine ? in_request % 16 : pool_row;
-        return mine ? own + n * paged_part_floats(16, D) : pre + (size_t)(n - own_parts) * pool_step * paged_part_floats(p.pool_height, D);
+        height = mine ? p.height : p.pool_height;
+        in_tile = mine ? in_request % p.height : pool_row;
+        return mine ? own + (size_t)n * own_step * paged_part_floats(p.height, D) : pre + (size_t)(n - own_parts) * pool_step * paged_part_floats(p.pool_height, D);
     };
     float m = -__builtin_inff(), l = 0, o[PER] = {};
     if (todo) {
@@ -954,10 +958,8 @@ hipError_t allow_paged()
 {
     hipError_t e = allow<64, 2, 3>();
     if (e == hipSuccess) e = allow<64, 4, 3>();
-    if (e == hipSuccess) e = allow<64, 8, 3>();
     if (e == hipSuccess) e = allow<128, 2, 2>();
     if (e == hipSuccess) e = allow<128, 4, 2>();
-    if (e == hipSuccess) e = allow<128, 8, 3>();
     return e;
 }
 
@@ -972,8 +974,8 @@ hipError_t launch_paged_few(const PagedArgs& a, bool bf16, int n_cu, hipStream_t
 
 hipError_t launch_paged_many(const PagedArgs& a, int height, hipStream_t s)
 {
-    if (a.head_dim > 64) return height == 256 ? go_many<128, 8, 3>(a, s) : height == 128 ? go_many<128, 4, 2>(a, s) : go_many<128, 2, 2>(a, s);
-    return height == 256 ? go_many<64, 8, 3>(a, s) : height == 128 ? go_many<64, 4, 3>(a, s) : go_many<64, 2, 3>(a, s);
+    if (a.head_dim > 64) return height == 128 ? go_many<128, 4, 2>(a, s) : go_many<128, 2, 2>(a, s);
+    return height == 128 ? go_many<64, 4, 3>(a, s) : go_many<64, 2, 3>(a, s);
 }
 
 hipError_t launch_paged_join(const PagedArgs& a, bool bf16, hipStream_t s)

@@ -112,7 +112,7 @@ inline void plan_paged_few(PagedArgs& a, const PagedCut& cut)
 {
     a.pooled = cut.pools != PagedPools::NONE && a.n_pools;
     a.share = a.pool_share = cut.share;
-    a.pool_height = PAGED_FEW_ROWS;
+    a.height = a.pool_height = PAGED_FEW_ROWS;
     const bool pools = a.pooled && cut.pools == PagedPools::TILES;
     long long items = 0;
     int most = 1;
@@ -221,32 +221,65 @@ inline void plan_paged_pools(PagedArgs& a, int height, int n_cu)
     plan_runs(a, a.pool_first, a.n_pools, [&](int g) { return std::pair<int, double>(tiles_of(g) * paged_parts(a.pool[g].len, a.pool_share), a.pool_share ? a.pool_share : a.pool[g].len); });
 }
 
-// Requests of many rows, gathered: the height of a tile.
-inline int plan_paged_many(PagedArgs& a, int n_cu)
+// Requests of many rows, gathered, in tiles of 128 over whole sequences or parts of them: a tile's 64 keys by themselves and with the compute unit full (one request of 512 and of 1024 rows,
+// 32 heads of 128 that share 8, 17.4 and 28.1 us; of 2048 behind 4096 187).  Tiles of 64, where requests have no more rows, are no faster (32 requests of up to 64 rows over up to 1230
+// 46.6 us, in tiles of 128 42.1; 64 of 64 over 300 22.1 / 22.4), nor are such of 256 (4 of 512 over 1024 40.7 / 42.6, 2 of 4096 289 / 294, one of 512 over 2560 72 / 56).
+constexpr int PAGED_MANY_HEIGHT = 128;
+struct PagedManyCosts { double start, alone, full; };
+constexpr PagedManyCosts paged_many_costs(int d) { return d == 128 ? PagedManyCosts{6500, 1250, 970} : PagedManyCosts{5500, 900, 690}; }
+inline double paged_keys(const PagedArgs& a, int i)      // that a tile of the i-th request takes on average
 {
-    constexpr int OWN = 160;             // a tile's own cost, in keys (measured for cross attention)
-    long long large = 0;
+    const int q = (a.row[i + 1] - a.row[i]) / (a.n_heads / a.n_kv_heads);
+    return paged_len(a, a.req[i]) - (a.causal ? std::min(q, own_len_of(a.req[i])) / 2 : 0);
+}
+// One request of 128 rows over 4224 keys takes 86 us whole and 29.7 in 8 parts, one of 512 over 2560 56 and 49.6 in two.
+inline PagedCut paged_many_cut(const PagedArgs& a, int n_cu, double unique)
+{
+    constexpr int height = PAGED_MANY_HEIGHT;
+    const int d = paged_width(a.head_dim);
+    const PagedManyCosts c = paged_many_costs(d);
+    const long long room = (long long)paged_room(a.n_kv_heads) * PAGED_FEW_ROWS / height;
+    const double held = d == 128 ? 2 : 3;
     int longest = 0;
+    double work = 0;                     // tiles' 64 keys
     for (int i = 0; i < a.n; ++i) {
-        large += (long long)(a.row[i + 1] - a.row[i] + 255) / 256 * a.n_kv_heads;
         longest = std::max(longest, paged_len(a, a.req[i]));
+        work += (double)((a.row[i + 1] - a.row[i] + height - 1) / height) * a.n_kv_heads * (paged_keys(a, i) / 64 + 1);
     }
-    const int height = longest >= 1024 && large >= n_cu - n_cu / 4 ? 256 : 128;
-    auto tiles_of = [&](int i) { return (a.row[i + 1] - a.row[i] + height - 1) / height * a.n_kv_heads; };
+    PagedCut best{PagedPools::NONE, 0, 1e30};
+    for (int parts = 1; parts <= 64; parts += std::max(1, parts / 4)) {
+        const int share = parts == 1 ? 0 : ((longest + parts - 1) / parts + 63) / 64 * 64;
+        if (parts > 1 && share < 128) break;
+        long long items = 0;
+        for (int i = 0; i < a.n; ++i) items += (long long)((a.row[i + 1] - a.row[i] + height - 1) / height) * a.n_kv_heads * paged_parts(paged_len(a, a.req[i]), share);
+        if (parts > 1 && items > room) break;
+        const double one = std::min<double>(items, n_cu * held) > n_cu ? std::max(c.alone, 2 * c.full) : c.alone;
+        const double bounds[3] = {c.start + ((share ? share : longest) + 63) / 64 * one, items > n_cu ? (work * c.full + items * c.start / held) / n_cu : 0, unique / 4800 + 2500};
+        double ns = 0;
+        for (double x : bounds) ns += x * x * x;
+        ns = std::cbrt(ns);
+        if (parts > 1) ns += 5000 + (double)a.rows * a.n_kv_heads * parts * 4 * (d + 2) * 2 / 3500;
+        if (ns < best.ns) best = PagedCut{PagedPools::NONE, share, ns};
+    }
+    return best;
+}
+inline void plan_paged_many(PagedArgs& a, const PagedCut& cut)
+{
+    constexpr int height = PAGED_MANY_HEIGHT;
+    constexpr int OWN = 160;             // a tile's own cost, in keys (measured for cross attention)
+    auto tiles_of = [&](int i) { return (a.row[i + 1] - a.row[i] + height - 1) / height * a.n_kv_heads * paged_parts(paged_len(a, a.req[i]), a.share); };
+    a.pooled = false;
+    a.share = a.pool_share = cut.share;
+    a.per = 0;
+    a.join = false;
+    a.height = a.pool_height = height;
     int at = 0;
     for (int i = 0; i < a.n; ++i) {
         a.req[i].first = at;
         at += tiles_of(i);
     }
-    a.share = a.pool_share = a.per = 0;
-    a.join = false;
-    a.pool_height = height;
     a.items = a.pool_first = at;
-    plan_runs(a, 0, a.n, [&](int i) {
-        const int q = (a.row[i + 1] - a.row[i]) / (a.n_heads / a.n_kv_heads);
-        return std::pair<int, double>(tiles_of(i), OWN + paged_len(a, a.req[i]) - (a.causal ? std::min(q, own_len_of(a.req[i])) / 2 : 0));
-    });
-    return height;
+    plan_runs(a, 0, a.n, [&](int i) { return std::pair<int, double>(tiles_of(i), OWN + paged_keys(a, i) / paged_parts(paged_len(a, a.req[i]), a.share)); });
 }
 
 }  // namespace tts

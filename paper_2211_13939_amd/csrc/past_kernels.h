@@ -96,7 +96,8 @@ struct PagedCommon {
     int q_first;                         // query row of the launch's first query, where they lie back to back; -1: they do not
     int items;                           // tiles of the launch
     int share, pool_share;               // length of a part of a request's keys, of a prefix's, 0: they have none
-    int pool_first, pool_height;         // first tile that is a prefix's; rows of such a tile
+    int pool_first;                      // first tile that is a prefix's
+    int height, pool_height;             // rows of a request's tile, of a prefix's
     bool causal;
     bool pooled;                         // prefixes have tiles of their own, over all their requests' rows; otherwise a request's keys begin with its prefix's
     bool join;                           // a row's last part to arrive joins them, in so many sums
@@ -131,7 +132,7 @@ constexpr size_t paged_part_floats(int rows, int d) { return (size_t)rows * (d +
 constexpr int paged_width(int head_dim) { return head_dim > 64 ? 128 : 64; }
 hipError_t allow_paged();                // once on each device, before the first launch there
 hipError_t launch_paged_few(const PagedArgs& a, bool bf16, int n_cu, hipStream_t s);     // tiles of 16 rows
-hipError_t launch_paged_many(const PagedArgs& a, int height, hipStream_t s);    // of 64, 128 or 256, two bytes
+hipError_t launch_paged_many(const PagedArgs& a, int height, hipStream_t s);    // of 64 or 128, two bytes
 hipError_t launch_paged_join(const PagedArgs& a, bool bf16, hipStream_t s);     // rows of requests that have a prefix apart or parts, where their last part does not join them
 
 }  // namespace tts
