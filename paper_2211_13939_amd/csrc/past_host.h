@@ -47,7 +47,7 @@ inline TurnAngles turn_angles(const tts_rotary_angles& a, int head_dim, const ui
 {
     const bool pairs = a.rot_dim && a.layout == TTS_ROTARY_PAIRS;
     const TurnShape s = turn_shape(head_dim, a.rot_dim, pairs);
-    return {freqs, (float)a.magnitude, a.rot_dim / 2, s.width, s.units, s.side, s.blocks, pairs};
+    return {freqs, (float)a.magnitude, a.rot_dim / 2, s.width, s.units, s.side, s.blocks, by_of((unsigned)s.units), pairs};
 }
 
 // Rows of `width` elements, `stride` apart (0: back to back).

@@ -5,20 +5,27 @@
 
 namespace tts {
 
+// x / y by 2^32 / y rounded up; y = 1: by 0.  Exact while x * y <= 2^32, for powers of two always.
+constexpr unsigned by_of(unsigned y) { return y <= 1 ? 0 : (unsigned)(((1ull << 32) + y - 1) / y); }
+constexpr unsigned NOT_BY = ~0u;         // (of no y)
+__host__ __device__ inline int over(int x, unsigned by)
+{
+    return by ? (int)(((unsigned long long)(unsigned)x * by) >> 32) : x;
+}
+
 // How heads are dealt to a wave's lanes: a unit is what a lane has of a head, two chunks of `width` columns.  Halves: chunks that lie rot_dim / 2 apart, then what does not turn in
-// neighbouring ones; pairs: neighbouring chunks of 4.  Heads of `units` units lie `side` to a wave; of more than 64, in `blocks` of 64.
+// neighbouring ones, the last of either so far back that it ends with them (what two lanes have they write alike); pairs: neighbouring chunks of 4.  Heads of `units` units lie `side` to a
+// wave; of more than 64, in `blocks` of 64, and then no two have the same of what turns: a call in place would turn it twice.
 struct TurnShape {
     int width, units, side, blocks;
 };
 inline TurnShape turn_shape(int head_dim, int rot_dim, bool pairs)
 {
     TurnShape s;
-    if (pairs || rot_dim == 0) {
-        s.width = pairs ? 4 : 8;
-        s.units = (head_dim + 2 * s.width - 1) / (2 * s.width);
-    } else {
-        s.width = rot_dim / 2 % 8 == 0 ? 8 : rot_dim / 2 % 4 == 0 ? 4 : rot_dim / 2 % 2 == 0 ? 2 : 1;
-        s.units = rot_dim / 2 / s.width + (head_dim - rot_dim + 2 * s.width - 1) / (2 * s.width);
+    const int half = rot_dim / 2, rest = head_dim - rot_dim;
+    for (s.width = pairs ? 4 : 8;; s.width /= 2) {
+        s.units = pairs ? (head_dim + 7) / 8 : (half + s.width - 1) / s.width + (rest + 2 * s.width - 1) / (2 * s.width);
+        if (pairs || s.width == 1 || ((!half || half >= s.width) && (!rest || rest >= s.width) && (half % s.width == 0 || s.units <= 64))) break;
     }
     s.side = s.units < 64 ? 64 / s.units : 1;
     s.blocks = (s.units + 63) / 64;
@@ -29,6 +36,7 @@ struct TurnAngles {
     const uint64_t* freqs;               // turns a position, times 2^64
     float magnitude;
     int half, width, units, side, blocks;    // half: rot_dim / 2
+    unsigned by_units;                   // for over()
     bool pairs;
 };
 struct RotaryArgs {
@@ -40,6 +48,7 @@ struct RotaryArgs {
     int rows, first, heads, head_dim;
     bool back;
     int per, jobs;                       // of a row: head steps of a wave, waves
+    unsigned by_jobs;                    // for over(), where that is exact
 };
 hipError_t launch_rotary(RotaryArgs& a, bool x_bf16, bool y_bf16, int n_cu, hipStream_t s);
 
@@ -56,6 +65,8 @@ struct AppendCommon {
     TurnAngles turn;
     int rows, n, heads, kv_heads, head_dim, n_pages, table_cols, page_shift;
     int per, k_jobs, v_jobs, q_jobs;     // of a row: head steps of a wave, waves
+    int each;                            // rows of every request, 0: they differ
+    unsigned by_each, by_jobs, by_v;     // for over() (by_jobs: where that is exact); v: lanes that a head takes
 };
 template <int N> struct AppendArgsOf : AppendCommon {
     static constexpr int BATCH = N;
@@ -104,13 +115,6 @@ struct PagedCommon {
     int subs;
     int start[9];                        // many rows: first of the tiles that each XCD takes
 };
-// x / y by 2^32 / y rounded up; y = 1: by 0.  Exact while x * y <= 2^32, for powers of two always.
-constexpr unsigned by_of(unsigned y) { return y <= 1 ? 0 : (unsigned)(((1ull << 32) + y - 1) / y); }
-constexpr unsigned NOT_BY = ~0u;         // (of no y)
-__host__ __device__ inline int over(int x, unsigned by)
-{
-    return by ? (int)(((unsigned long long)(unsigned)x * by) >> 32) : x;
-}
 template <int N> struct PagedArgsOf : PagedCommon {
     static constexpr int BATCH = N, POOLS = N < PAGED_POOLS ? N : PAGED_POOLS;
     PagedReq req[N];

@@ -15,26 +15,24 @@ namespace {
 
 constexpr int WAVES = 4, AHEAD = 4;      // of a workgroup; heads whose loads are on their way together
 
+// V columns of a head from any on: an address is aligned to an element (the hardware takes wide accesses at any).
 template <typename T, int V> struct Words {
     static constexpr int BYTES = V * (int)sizeof(T), N = BYTES < 4 ? 1 : BYTES / 4;
+    struct __attribute__((packed, aligned(sizeof(T)))) Piece { uint32_t w[BYTES < 16 ? N : 4]; };
     uint32_t w[N];
     __device__ __forceinline__ void load(const T* at)
     {
         if constexpr (BYTES == 2) w[0] = reinterpret_cast<const uint16_t*>(at)[0];
-        else if constexpr (BYTES == 4) w[0] = reinterpret_cast<const uint32_t*>(at)[0];
-        else if constexpr (BYTES == 8) *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(at);
         else
 #pragma unroll
-            for (int i = 0; i < BYTES / 16; ++i) *reinterpret_cast<uint4*>(w + 4 * i) = reinterpret_cast<const uint4*>(at)[i];
+            for (int i = 0; i < (BYTES + 15) / 16; ++i) reinterpret_cast<Piece*>(w)[i] = reinterpret_cast<const Piece*>(at)[i];
     }
     __device__ __forceinline__ void store(T* at) const
     {
         if constexpr (BYTES == 2) reinterpret_cast<uint16_t*>(at)[0] = (uint16_t)w[0];
-        else if constexpr (BYTES == 4) reinterpret_cast<uint32_t*>(at)[0] = w[0];
-        else if constexpr (BYTES == 8) *reinterpret_cast<uint2*>(at) = *reinterpret_cast<const uint2*>(w);
         else
 #pragma unroll
-            for (int i = 0; i < BYTES / 16; ++i) reinterpret_cast<uint4*>(at)[i] = *reinterpret_cast<const uint4*>(w + 4 * i);
+            for (int i = 0; i < (BYTES + 15) / 16; ++i) reinterpret_cast<Piece*>(at)[i] = reinterpret_cast<const Piece*>(w)[i];
     }
     __device__ __forceinline__ float get(int i) const
     {
@@ -72,13 +70,12 @@ __device__ __forceinline__ void sine_cosine(int position, uint64_t freq, float& 
 // A lane's unit of a head: its columns and their angles.  V: columns of a chunk.
 template <int V, bool PAIRS> struct Unit {
     static constexpr int PAIRS_OF = V;
-    int a, b;                            // first columns of the two chunks
+    int a, b, first;                     // first columns of the two chunks; the first of the lane's pairs
     bool on[PAIRS ? V : 1];              // whether they turn
     float c[V], s[V];
-    __device__ __forceinline__ Unit(const TurnAngles& t, int unit, int position, bool back, int head_dim)
+    __device__ __forceinline__ Unit(const TurnAngles& t, int unit, int head_dim)
     {
-        const int turning = t.half / V;
-        int first;                       // of the lane's pairs
+        const int turning = (t.half + V - 1) / V;
         if constexpr (PAIRS) {
             a = 2 * V * unit;
             b = a + V;
@@ -87,15 +84,18 @@ template <int V, bool PAIRS> struct Unit {
             for (int i = 0; i < V; ++i) on[i] = first + i < t.half;
         } else {
             on[0] = unit < turning;
+            first = min(V * unit, t.half - V);
             const int rest = 2 * t.half + 2 * V * (unit - turning);
-            a = on[0] ? V * unit : rest;
-            b = on[0] ? t.half + V * unit : rest + V < head_dim ? rest + V : rest;     // (a chunk that there is not: the first again)
-            first = V * unit;
+            a = on[0] ? first : min(rest, head_dim - V);
+            b = on[0] ? t.half + first : min(rest + V, head_dim - V);
         }
+    }
+    __device__ __forceinline__ void angles(const TurnAngles& t, int position, bool back)
+    {
         const float sign = back ? -t.magnitude : t.magnitude;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            sine_cosine(position, t.half ? t.freqs[min(first + i, t.half - 1)] : 0, s[i], c[i]);
+            sine_cosine(position, t.half ? t.freqs[max(0, min(first + i, t.half - 1))] : 0, s[i], c[i]);
             c[i] *= t.magnitude;
             s[i] *= sign;
         }
@@ -128,13 +128,16 @@ template <int V, bool PAIRS> struct Unit {
     }
 };
 
-// Head steps from .. to of a wave: `side` heads each, a lane's unit of one of them.
-template <typename TX, typename TY, int V, bool PAIRS>
-__device__ __forceinline__ void turn_heads(const TurnAngles& t, const TX* x, TY* y, int x_apart, int y_apart, int heads, int from, int to, int block, int position, bool back, int head_dim)
+// Where a wave's rows go, and at which position they are; y null: nowhere.
+template <typename TY> struct To { TY* y; int position; };
+// Head steps from .. to of a wave: `side` heads each, a lane's unit of one of them.  `where` says where they go, when the first are on their way: a new row's page takes two trips to memory.
+template <typename TX, typename TY, int V, bool PAIRS, typename Where>
+__device__ __forceinline__ void turn_heads(const TurnAngles& t, const TX* x, int x_apart, int y_apart, int heads, int from, int to, int block, bool back, int head_dim, Where where)
 {
-    const int lane = threadIdx.x & 63, in_side = t.units < 64 ? lane / t.units : 0, unit = t.units < 64 ? lane % t.units : 64 * block + lane;
+    const int lane = threadIdx.x & 63, in_side = over(lane, t.by_units), unit = t.units < 64 ? lane - in_side * t.units : 64 * block + lane;
     if (in_side >= t.side || unit >= t.units) return;
-    const Unit<V, PAIRS> u(t, unit, position, back, head_dim);
+    Unit<V, PAIRS> u(t, unit, head_dim);
+    TY* y = nullptr;
     for (int at = from; at < to; at += AHEAD) {
         Words<TX, V> xa[AHEAD], xb[AHEAD];
 #pragma unroll
@@ -142,6 +145,12 @@ __device__ __forceinline__ void turn_heads(const TurnAngles& t, const TX* x, TY*
             const TX* from_head = x + (long long)min((at + i) * t.side + in_side, heads - 1) * x_apart;
             xa[i].load(from_head + u.a);
             xb[i].load(from_head + u.b);
+        }
+        if (at == from) {
+            const To<TY> place = where();
+            if (!place.y) return;
+            y = place.y;
+            u.angles(t, place.position, back);
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
@@ -155,52 +164,72 @@ __device__ __forceinline__ void turn_heads(const TurnAngles& t, const TX* x, TY*
     }
 }
 
-template <typename TX, typename TY>
-__device__ __forceinline__ void copy_heads(const TX* x, TY* y, int x_apart, int y_apart, int heads, int from, int to, int head_dim)
+template <typename TX, typename TY, typename Where>
+__device__ __forceinline__ void copy_heads(const TX* x, int x_apart, int y_apart, int heads, int from, int to, int head_dim, unsigned by_units, Where where)
 {
-    const int lane = threadIdx.x & 63, units = head_dim / 8, side = 64 / units, in_side = lane / units, column = lane % units * 8;
+    const int lane = threadIdx.x & 63, units = head_dim / 8, in_side = over(lane, by_units), column = (lane - in_side * units) * 8, side = over(64, by_units);
     if (in_side >= side) return;
+    TY* y = nullptr;
     for (int at = from; at < to; at += AHEAD) {
         Words<TX, 8> in[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) in[i].load(x + (long long)min((at + i) * side + in_side, heads - 1) * x_apart + column);
+        if (at == from) {
+            y = where().y;
+            if (!y) return;
+        }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int head = (at + i) * side + in_side;
             if (at + i >= to || head >= heads) break;
-            Words<TY, 8> out;
-            if constexpr (std::is_same<TX, TY>::value) out = in[i];
+            if constexpr (std::is_same<TX, TY>::value) in[i].store(y + (long long)head * y_apart + column);
             else {
                 float f[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = in[i].get(j);
+                Words<TY, 8> out;
                 out.set(f);
+                out.store(y + (long long)head * y_apart + column);
             }
-            out.store(y + (long long)head * y_apart + column);
         }
     }
 }
+
+// (a row's waves, `blocks` of them over the same heads)
+__device__ __forceinline__ int row_of(long long at, int jobs, unsigned by) { return by != NOT_BY ? over((int)at, by) : (int)(at / jobs); }
+__device__ __forceinline__ int from_of(int job, int blocks) { return blocks == 1 ? job : job / blocks; }
 
 template <typename TX, typename TY, int V, bool PAIRS> __global__ __launch_bounds__(64 * WAVES) void k_rotary(RotaryArgs p)
 {
     const long long all = (long long)p.rows * p.jobs, waves = (long long)gridDim.x * WAVES;
     for (long long at = (long long)blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); at < all; at += waves) {
-        const int row = (int)(at / p.jobs), job = (int)(at - (long long)row * p.jobs), block = job % p.turn.blocks, from = job / p.turn.blocks * p.per;
+        const int row = row_of(at, p.jobs, p.by_jobs), job = (int)(at - (long long)row * p.jobs), step = from_of(job, p.turn.blocks), from = step * p.per;
         const int steps = (p.heads + p.turn.side - 1) / p.turn.side;
-        const int position = p.positions ? p.positions[row] : p.first + row;
-        turn_heads<TX, TY, V, PAIRS>(p.turn, static_cast<const TX*>(p.x) + row * p.x_stride, static_cast<TY*>(p.y) + row * p.y_stride, p.head_dim, p.head_dim, p.heads, from, min(from + p.per, steps),
-                                     block, position, p.back, p.head_dim);
+        turn_heads<TX, TY, V, PAIRS>(p.turn, static_cast<const TX*>(p.x) + row * p.x_stride, p.head_dim, p.head_dim, p.heads, from, min(from + p.per, steps), job - step * p.turn.blocks, p.back,
+                                     p.head_dim, [&] { return To<TY>{static_cast<TY*>(p.y) + row * p.y_stride, p.positions ? p.positions[row] : p.first + row}; });
     }
 }
 
-// The request that row `row` of a launch is of.
-template <typename Args> __device__ __forceinline__ int request_of_row(const Args& p, int row)
+// The request that row `row` of a launch is of.  (One trip to the arguments, which are far.)
+template <typename Args> __device__ __forceinline__ AppendReq request_of_row(const Args& p, int row)
 {
+    if (p.each) return p.req[over(row, p.by_each)];
     const int lane = threadIdx.x & 63;
+    AppendReq mine[(Args::BATCH + 63) / 64];
     int before = 0;
 #pragma unroll
-    for (int i = 0; i < Args::BATCH; i += 64) before += __popcll(__ballot(i + lane < p.n && p.req[min(i + lane, p.n - 1)].first <= row));
-    return __builtin_amdgcn_readfirstlane(before) - 1;
+    for (int i = 0; i < Args::BATCH; i += 64) mine[i / 64] = p.req[min(i + lane, p.n - 1)];
+#pragma unroll
+    for (int i = 0; i < Args::BATCH; i += 64) before += __popcll(__ballot(i + lane < p.n && mine[i / 64].first <= row));
+    const int at = __builtin_amdgcn_readfirstlane(before) - 1;
+    AppendReq r = {};
+#pragma unroll
+    for (int i = 0; i < Args::BATCH; i += 64)
+        if (at >> 6 == i / 64) {
+            const AppendReq& m = mine[i / 64];
+            r = {__builtin_amdgcn_readlane(m.first, at & 63), __builtin_amdgcn_readlane(m.row, at & 63), __builtin_amdgcn_readlane(m.table_row, at & 63), __builtin_amdgcn_readlane(m.position, at & 63)};
+        }
+    return r;
 }
 
 template <typename TX, typename TY, int V, bool PAIRS, typename Args> __global__ __launch_bounds__(64 * WAVES) void k_append(Args p)
@@ -208,29 +237,32 @@ template <typename TX, typename TY, int V, bool PAIRS, typename Args> __global__
     const int jobs = p.k_jobs + p.v_jobs + p.q_jobs;
     const long long all = (long long)p.rows * jobs, waves = (long long)gridDim.x * WAVES;
     for (long long at = (long long)blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); at < all; at += waves) {
-        const int row = (int)(at / jobs);
+        const int row = row_of(at, jobs, p.by_jobs);
         int job = (int)(at - (long long)row * jobs);
-        const AppendReq r = p.req[request_of_row(p, row)];
-        const int cache_row = r.row + (row - r.first), position = r.position + (row - r.first);
-        if (job >= p.k_jobs + p.v_jobs) {
-            job -= p.k_jobs + p.v_jobs;
-            const int from = job / p.turn.blocks * p.per, steps = (p.heads + p.turn.side - 1) / p.turn.side;
-            turn_heads<TX, TY, V, PAIRS>(p.turn, static_cast<const TX*>(p.q) + row * p.q_stride, static_cast<TY*>(p.q_out) + row * p.q_out_stride, p.head_dim, p.head_dim, p.heads, from,
-                                         min(from + p.per, steps), job % p.turn.blocks, position, false, p.head_dim);
+        const AppendReq r = request_of_row(p, row);
+        const int position = r.position + (row - r.first), apart = p.head_dim << p.page_shift;
+        auto in_page = [&](void* pages) {
+            const int cache_row = r.row + (row - r.first), page = p.table[(long long)r.table_row * p.table_cols + (cache_row >> p.page_shift)];
+            // (no page: the row is not kept)
+            TY* y = (unsigned)page < (unsigned)p.n_pages ? static_cast<TY*>(pages) + page * p.page_stride + (long long)(cache_row & ((1 << p.page_shift) - 1)) * p.head_dim : nullptr;
+            return To<TY>{y, position};
+        };
+        if (job < p.k_jobs) {
+            const int step = from_of(job, p.turn.blocks), from = step * p.per, steps = (p.kv_heads + p.turn.side - 1) / p.turn.side;
+            turn_heads<TX, TY, V, PAIRS>(p.turn, static_cast<const TX*>(p.k) + row * p.k_stride, p.head_dim, apart, p.kv_heads, from, min(from + p.per, steps), job - step * p.turn.blocks, false,
+                                         p.head_dim, [&] { return in_page(p.k_pages); });
             continue;
         }
-        const int page = p.table[(long long)r.table_row * p.table_cols + (cache_row >> p.page_shift)];
-        if ((unsigned)page >= (unsigned)p.n_pages) continue;                                // (no page: the row is not kept)
-        const int apart = p.head_dim << p.page_shift;
-        const long long to = page * p.page_stride + (long long)(cache_row & ((1 << p.page_shift) - 1)) * p.head_dim;
-        if (job < p.k_jobs) {
-            const int from = job / p.turn.blocks * p.per, steps = (p.kv_heads + p.turn.side - 1) / p.turn.side;
-            turn_heads<TX, TY, V, PAIRS>(p.turn, static_cast<const TX*>(p.k) + row * p.k_stride, static_cast<TY*>(p.k_pages) + to, p.head_dim, apart, p.kv_heads, from, min(from + p.per, steps),
-                                         job % p.turn.blocks, position, false, p.head_dim);
-        } else {
-            const int from = (job - p.k_jobs) * p.per, side = 64 / (p.head_dim / 8), steps = (p.kv_heads + side - 1) / side;
-            copy_heads(static_cast<const TX*>(p.v) + row * p.v_stride, static_cast<TY*>(p.v_pages) + to, p.head_dim, apart, p.kv_heads, from, min(from + p.per, steps), p.head_dim);
+        job -= p.k_jobs;
+        if (job < p.v_jobs) {
+            const int from = job * p.per, side = over(64, p.by_v), steps = (p.kv_heads + side - 1) / side;
+            copy_heads<TX, TY>(static_cast<const TX*>(p.v) + row * p.v_stride, p.head_dim, apart, p.kv_heads, from, min(from + p.per, steps), p.head_dim, p.by_v, [&] { return in_page(p.v_pages); });
+            continue;
         }
+        job -= p.v_jobs;
+        const int step = from_of(job, p.turn.blocks), from = step * p.per, steps = (p.heads + p.turn.side - 1) / p.turn.side;
+        turn_heads<TX, TY, V, PAIRS>(p.turn, static_cast<const TX*>(p.q) + row * p.q_stride, p.head_dim, p.head_dim, p.heads, from, min(from + p.per, steps), job - step * p.turn.blocks, false,
+                                     p.head_dim, [&] { return To<TY>{static_cast<TY*>(p.q_out) + row * p.q_out_stride, position}; });
     }
 }
 
@@ -251,6 +283,7 @@ template <typename F> hipError_t with_unit(const TurnAngles& t, F f)
     }
 }
 
+unsigned by_jobs_of(long long rows, int jobs) { return rows * jobs * jobs <= 1LL << 32 ? by_of((unsigned)jobs) : NOT_BY; }
 int steps_of(int heads, int side) { return (heads + side - 1) / side; }
 unsigned grid_of(long long waves) { return (unsigned)std::min<long long>((waves + WAVES - 1) / WAVES, 1 << 20); }
 
@@ -261,6 +294,7 @@ hipError_t launch_rotary(RotaryArgs& a, bool x_bf16, bool y_bf16, int n_cu, hipS
     const int steps = steps_of(a.heads, a.turn.side);
     a.per = (long long)a.rows * steps * a.turn.blocks <= 16 * n_cu ? 1 : steps;
     a.jobs = (steps + a.per - 1) / a.per * a.turn.blocks;
+    a.by_jobs = by_jobs_of(a.rows, a.jobs);
     return with_types(x_bf16, y_bf16, [&](auto x, auto y) {
         return with_unit(a.turn, [&](auto width, auto pairs) {
             hipLaunchKernelGGL((k_rotary<decltype(x), decltype(y), decltype(width)::value, decltype(pairs)::value>), dim3(grid_of((long long)a.rows * a.jobs)), dim3(64 * WAVES), 0, s, a);
@@ -276,6 +310,13 @@ hipError_t launch_append(AppendArgs& a, bool x_bf16, bool bf16, int n_cu, hipStr
     a.k_jobs = (k_steps + a.per - 1) / a.per * a.turn.blocks;
     a.q_jobs = (q_steps + a.per - 1) / a.per * a.turn.blocks;
     a.v_jobs = (v_steps + a.per - 1) / a.per;
+    a.by_v = by_of((unsigned)a.head_dim / 8);
+    a.by_jobs = by_jobs_of(a.rows, a.k_jobs + a.q_jobs + a.v_jobs);
+    a.each = a.n > 1 ? a.req[1].first : a.rows;
+    for (int i = 0; i < a.n; ++i)
+        if (a.each && (a.req[i].first != (long long)i * a.each || a.rows != (long long)a.n * a.each)) a.each = 0;
+    if ((long long)a.rows * a.each > 1LL << 32) a.each = 0;
+    a.by_each = by_of((unsigned)a.each);
     const unsigned grid = grid_of((long long)a.rows * (a.k_jobs + a.q_jobs + a.v_jobs));
     return with_types(x_bf16, bf16, [&](auto x, auto y) {
         return with_unit(a.turn, [&](auto width, auto pairs) {

@@ -193,3 +193,11 @@ def test_no_rows():
     torch.cuda.synchronize()
     assert (pages == 1).all()
     op.close()
+
+
+@pytest.mark.parametrize("x_bf16,bf16", [(True, True), (False, True), (False, False)])
+@pytest.mark.parametrize("n,each", [(20, 5), (130, 1), (7, 64), (128, 3), (1, 300), (200, 2)])
+def test_requests_of_as_many_rows_each(n, each, x_bf16, bf16):
+    import torch
+    say(f"case append {n} requests of {each} rows {x_bf16} {bf16}")
+    _run(torch, 2, 4, 96, 16, 26, False, x_bf16, bf16, [each] * n, [(13 * i) % 50 for i in range(n)], seed=n)

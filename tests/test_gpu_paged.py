@@ -320,3 +320,13 @@ def test_nothing_to_do_and_nothing_to_see():
         assert (out == 0).all() and torch.isneginf(lse).all()
         out.fill_(1)
     op.close()
+
+
+@pytest.mark.parametrize("n,heads,kv,d,page,q,past,causal", [(1, 8, 2, 128, 16, 128, 3000, True), (1, 4, 1, 64, 64, 300, 1500, True), (2, 8, 8, 40, 16, 150, 2000, False), (3, 16, 2, 72, 32, 40, 2500, True),
+                                                            (1, 4, 4, 128, 128, 700, 900, False)])
+def test_parts_of_many_rows(n, heads, kv, d, page, q, past, causal):
+    """Tiles of many rows over parts of their sequences, of which some see nothing of the last ones; prefixes ahead; pages that there are not; joined by a launch behind them."""
+    import torch
+    q_len, prefix = [max(1, q - 31 * i) for i in range(n)], [0] * n if n > 1 else None
+    own = [past + a - 17 * i for i, a in enumerate(q_len)]
+    Case(torch, heads, kv, d, page, True, q_len, own, prefix, [100] if prefix else [], gone=[(0, 3), (0, 0)], seed=d + q, causal=causal).check()

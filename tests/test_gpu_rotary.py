@@ -164,3 +164,14 @@ def test_no_rows():
     op.run_device(x, x)
     torch.cuda.synchronize()
     op.close()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("d,rot", [(96, 26), (64, 54), (64, 62), (40, 14), (256, 254), (256, 252), (256, 250), (256, 14), (248, 10), (256, 2)])
+def test_halves_that_end_inside_a_chunk(d, rot, bf16):
+    """Columns that two lanes have are turned once, in place too, and those that do not turn stay."""
+    import torch
+    say(f"case rotary {rot} of {d} in place {bf16}")
+    for rows, heads in ((1, 1), (9, 3), (300, 6)):
+        _run(torch, rows, heads, d, rot, False, bf16, bf16, first=77, in_place=True, seed=d + rot + rows)
+        _run(torch, rows, heads, d, rot, False, not bf16, bf16, first=77, seed=d + rot + rows)
