@@ -17,22 +17,32 @@ constexpr int WAVES = 4, AHEAD = 4;      // of a workgroup; heads whose loads ar
 
 // V columns of a head from any on: an address is aligned to an element (the hardware takes wide accesses at any).
 template <typename T, int V> struct Words {
-    static constexpr int BYTES = V * (int)sizeof(T), N = BYTES < 4 ? 1 : BYTES / 4;
-    struct __attribute__((packed, aligned(sizeof(T)))) Piece { uint32_t w[BYTES < 16 ? N : 4]; };
+    static constexpr int BYTES = V * (int)sizeof(T), N = BYTES < 4 ? 1 : BYTES / 4, PIECE = BYTES < 16 ? N : 4;
+    typedef uint32_t Piece __attribute__((ext_vector_type(PIECE)));
+    typedef Piece Anywhere __attribute__((aligned(sizeof(T))));
     uint32_t w[N];
     __device__ __forceinline__ void load(const T* at)
     {
         if constexpr (BYTES == 2) w[0] = reinterpret_cast<const uint16_t*>(at)[0];
         else
 #pragma unroll
-            for (int i = 0; i < (BYTES + 15) / 16; ++i) reinterpret_cast<Piece*>(w)[i] = reinterpret_cast<const Piece*>(at)[i];
+            for (int i = 0; i < N / PIECE; ++i) {
+                const Piece x = reinterpret_cast<const Anywhere*>(at)[i];
+#pragma unroll
+                for (int j = 0; j < PIECE; ++j) w[PIECE * i + j] = x[j];
+            }
     }
     __device__ __forceinline__ void store(T* at) const
     {
         if constexpr (BYTES == 2) reinterpret_cast<uint16_t*>(at)[0] = (uint16_t)w[0];
         else
 #pragma unroll
-            for (int i = 0; i < (BYTES + 15) / 16; ++i) reinterpret_cast<Piece*>(at)[i] = reinterpret_cast<const Piece*>(w)[i];
+            for (int i = 0; i < N / PIECE; ++i) {
+                Piece x;
+#pragma unroll
+                for (int j = 0; j < PIECE; ++j) x[j] = w[PIECE * i + j];
+                reinterpret_cast<Anywhere*>(at)[i] = x;
+            }
     }
     __device__ __forceinline__ float get(int i) const
     {
