@@ -432,6 +432,11 @@ struct Parts {
 };
 
 // A tile of 16 rows over a part of its sequence; the waves take steps of keys in turn, the next one's on its way, and meet in LDS.
+//
+// Bound by latency: from the launch to the first step's scores lie three dependent trips to memory (arguments, a page's number, keys), 3.2 us with the way out; then a step of 32 keys takes
+// a wave what 16 KB take from wherever they are, and many of them the memory's rate (16 requests over 3000 to 9000 rows, 16 heads of 128 that share 4: 40 us, 4.0 TB/s; a short one by itself
+// 7.2). One step's registers, whose keys and values are asked for again as they are used up, leave room for 3 or 4 workgroups a compute unit; two steps' in turn were 20 KB of code and
+// slower (15.2 against 12.8 us over 30 drawn calls). A workgroup has eight waves while that leaves no compute unit without one: their steps in turn are a shorter way through a sequence.
 template <typename T, int D, bool FULL, int WAVES, typename Args> __global__ __launch_bounds__(WAVES * 64, D == 128 ? (WAVES == 4 && sizeof(T) == 2 ? 3 : 2) : 4) void k_paged_few(Args p)
 {
     using G = Geometry<T, D>;
@@ -618,6 +623,12 @@ template <typename T, int D, bool FULL, int WAVES, typename Args> __global__ __l
 
 // Many rows, two bytes: 32 * NW rows, 32 a wave, over the keys in tiles of 64 that all waves read from LDS while the next R - 1 are on their way there, 16 bytes a lane straight from
 // memory; one barrier a tile.  Where 64 tiles' keys lie, and which there are, is looked up at once and kept in LDS.
+//
+// Bound by the matrix pipe's and the softmax's turns, one behind the other in a wave: a tile's 64 keys take a workgroup of 128 rows by itself 1.25 us (columns 128; 64: 0.9), two of them a
+// compute unit 0.97 each (three of 64: 0.69), 1.1 PFLOP/s of the pipe's 2.5 (8 prompts of 1500 to 4000 behind a prefix of 500, 16 heads of 128 that share 4: 478 us, 0.88 over the scores
+// that count). A second workgroup a compute unit is worth more than taller tiles (2 slots of 32 KB and 232 registers leave room for it): 256 rows, three slots, took 289 us for 2 requests of
+// 4096 where 128 take 294, but 72 against 56 for one of 512 over 2560. All waves take all of the workgroup's tiles: skipping those that a wave's rows do not see made the compiler keep every
+// sum twice (copies and spilled registers: the prompts 588 us, and copies that now and then came too early where two workgroups shared a compute unit).
 template <int D, int NW, int R> struct PagedMany {
     static constexpr int ROW = 2 * D, PART = KEYS * ROW, SLOT = 2 * PART, LOADS = PART / 1024 / NW, AHEAD = 64, SIXTEENS = 2 * AHEAD * KEYS / 16;
     static constexpr int LDS = R * SLOT + SIXTEENS * 10 + 16;            // 8 bytes for where 16 keys lie, 2 for which of them there are; whether a value was taken out
@@ -630,7 +641,7 @@ __device__ __forceinline__ void to_lds_from(const char* base, uint32_t offset, u
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" : "={m0}"(m0) : "s"(to), "v"(offset), "s"(base) : "memory");
 }
 
-template <int D, int NW, int R, bool FULL, typename Args> __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : NW == 8 ? 4 : 3) void k_paged_many(Args p)
+template <int D, int NW, int R, bool FULL, typename Args> __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 3) void k_paged_many(Args p)
 {
     using M = PagedMany<D, NW, R>;
     constexpr int ROW = M::ROW, NK = D / 16, HEIGHT = 32 * NW;
@@ -691,19 +702,11 @@ template <int D, int NW, int R, bool FULL, typename Args> __global__ __launch_bo
         const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)x), high = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
         return (uint64_t)high << 32 | low;
     };
-    // where a tile's keys lie that this wave brings (asked for ahead: a trip to LDS for each would stand in every tile's way)
-    struct Froms { uint64_t at[M::LOADS]; };
-    auto ask = [&](int tile) {
-        Froms f;
-#pragma unroll
-        for (int i = 0; i < M::LOADS; ++i) f.at[i] = (uint64_t)where[(tile * (KEYS / 16) + (wave + i * NW) * 1024 / ROW / 16) % M::SIXTEENS];
-        return f;
-    };
     auto ask_which = [&](int tile) { return *reinterpret_cast<const uint64_t*>(which + tile * (KEYS / 16) % M::SIXTEENS); };
-    auto bring = [&](const Froms& f, int slot) {
+    auto bring = [&](int tile, int slot) {
         uint64_t from[M::LOADS];
 #pragma unroll
-        for (int i = 0; i < M::LOADS; ++i) from[i] = same(f.at[i]);
+        for (int i = 0; i < M::LOADS; ++i) from[i] = same((uint64_t)where[(tile * (KEYS / 16) + (wave + i * NW) * 1024 / ROW / 16) % M::SIXTEENS]);
 #pragma unroll
         for (int i = 0; i < M::LOADS; ++i) {
             const uint32_t to = lds_at + slot * M::SLOT + (wave + i * NW) * 1024;
@@ -715,7 +718,7 @@ template <int D, int NW, int R, bool FULL, typename Args> __global__ __launch_bo
         for (int i = threadIdx.x; i < R * M::SLOT / 16; i += 64 * NW) reinterpret_cast<uint4*>(lds)[i] = make_uint4(0, 0, 0, 0);
     if (threadIdx.x == 0) *odd = 0;
     __syncthreads();
-    for (int i = 0; i < R - 1 && first_tile + i < n_tiles; ++i) bring(ask(first_tile + i), i);
+    for (int i = 0; i < R - 1 && first_tile + i < n_tiles; ++i) bring(first_tile + i, i);
     uint64_t next_which = ask_which(first_tile);
     // The queries are here, with the first tile: waited for in the loop, they would be together with the tiles that are on their way.
 #pragma unroll
@@ -728,7 +731,7 @@ template <int D, int NW, int R, bool FULL, typename Args> __global__ __launch_bo
             look(tile + M::AHEAD / 2);
             __syncthreads();
         }
-        if (tile + R - 1 < n_tiles) bring(ask(tile + R - 1), free);
+        if (tile + R - 1 < n_tiles) bring(tile + R - 1, free);
         const uint64_t mask = same(next_which);
         next_which = ask_which(tile + 1);
         const char* keys = lds + slot * M::SLOT;

@@ -222,7 +222,7 @@ inline void plan_paged_pools(PagedArgs& a, int height, int n_cu)
 }
 
 // Requests of many rows, gathered, in tiles of 128 over whole sequences or parts of them: a tile's 64 keys by themselves and with the compute unit full (one request of 512 and of 1024 rows,
-// 32 heads of 128 that share 8, 17.4 and 28.1 us; of 2048 behind 4096 187).  Tiles of 64, where requests have no more rows, are no faster (32 requests of up to 64 rows over up to 1230
+// 32 heads of 128 that share 8, 17.4 and 28.1 us; of 2048 behind 4096 187).  Tiles of 64, where requests have no more rows, are no faster (32 requests of 40 rows over 700 to 2400
 // 46.6 us, in tiles of 128 42.1; 64 of 64 over 300 22.1 / 22.4), nor are such of 256 (4 of 512 over 1024 40.7 / 42.6, 2 of 4096 289 / 294, one of 512 over 2560 72 / 56).
 constexpr int PAGED_MANY_HEIGHT = 128;
 struct PagedManyCosts { double start, alone, full; };

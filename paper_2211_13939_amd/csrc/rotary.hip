@@ -3,6 +3,11 @@
 // Bound by memory: every element is read and written once.  A lane has the angles of its columns and takes them through several heads of its row, so that forming them costs
 // little: an angle is position * frequency in turns, as 64-bit fixed point, of which the product's low bits are what is left of whole turns, exact
 // for every position; of that the nearest quarter of a turn is a change of signs and places, and the rest, 1/8 of a turn at most, goes into the series of sine and cosine.
+//
+// Measured: 16384 rows of 40 heads of 128 in bf16 take what memory does (64 us, 5.3 TB/s), 16000 rows on their way into a cache with their queries 86 us (5.0 TB/s); small calls a launch and the trips that
+// depend on each other (one row 2.7 us; 64 requests' rows 3.8: arguments, table, store, with rows and angles asked for meanwhile).  What a lane takes through registers are vectors: pieces copied as structs went
+// through scratch memory, or were copied when they were stored (64 rows 8.0 us, 16000 101).  A head whose turning columns are no multiple of 16 has its last pieces overlap (of 26 columns of 96: single
+// columns took 20 us for 2778 rows of 4 heads, pieces of 8 columns 12.7).  Far from memory's rate: few heads of few columns, where a wave's lanes are not all used (one head of k and v: 10 of 64).
 #include "past_kernels.h"
 #include "mfma.h"
 
