@@ -132,3 +132,71 @@ def test_a_step_in_a_graph(bf16):
         torch.cuda.synchronize()
         assert torch.equal(b["out"], e["out"]) and torch.equal(b["lse"], e["lse"]) and torch.equal(b["q"], e["q"]), i
         assert torch.equal(got_k, kp) and torch.equal(got_v, vp), i
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    """Another device, type or number of elements, rows that do not lie back to back, arrays that come together: before anything is queued."""
+    import torch
+    heads, kv, d, page = 4, 2, 64, 16
+    cache = binding.Cache(binding.make_cache_config(kv, d, page, binding.make_rotary_angles(d), n_heads=heads, bf16=True, x_bf16=True))
+    attend = binding.PagedAttention(binding.make_paged_config(heads, kv, d, page, True))
+    rotary = binding.Rotary(binding.make_rotary_config(heads, d, binding.make_rotary_angles(d), True, True))
+    z = lambda *shape, **k: torch.zeros(shape, **{"dtype": torch.bfloat16, "device": "cuda:0", **k})             # noqa: E731
+    good = dict(k=z(3, kv, d), v=z(3, kv, d), k_pages=z(2, kv, page, d), v_pages=z(2, kv, page, d), table=z(1, 2, dtype=torch.int32), q=z(3, heads, d), q_out=z(3, heads, d))
+    bad = [dict(k=z(3, kv, d, device="cpu")), dict(k=z(3, kv, d, device="meta")), dict(v=z(3, kv, d, dtype=torch.float32)), dict(k=z(2, kv, d)), dict(k=z(3, d, kv).transpose(1, 2)), dict(q=None),
+           dict(q_out=z(3, heads, d, dtype=torch.float32)), dict(k_pages=z(2, kv, page, d, dtype=torch.float16)), dict(v_pages=z(1, kv, page, d)), dict(k_pages=z(2, page, kv, d).transpose(1, 2)),
+           dict(k_pages=z(3, kv, page, d + 8)[:, :, :, :d]), dict(table=z(1, 2, dtype=torch.int64)), dict(table=z(2, dtype=torch.int32)), dict(table=z(1, 4, dtype=torch.int32)[:, ::2]),
+           dict(v_pages=z(4, kv, page, d)[::2])]
+    batch = cache.batch([3], [0], [0])
+    cache.run_device(batch, **good)
+    for change in bad:
+        with pytest.raises(ValueError):
+            cache.run_device(batch, **{**good, **change})
+    good = dict(q=z(3, heads, d), k_pages=good["k_pages"], v_pages=good["v_pages"], table=good["table"], out=z(3, heads, d), lse=z(3, heads, dtype=torch.float32))
+    batch = attend.batch([3], [3], [0])
+    attend.run_device(batch, **good)
+    for change in [dict(q=z(3, heads, d, device="cpu")), dict(out=z(3, heads, d, dtype=torch.float32)), dict(out=z(4, heads, d)), dict(q=z(heads, 3, d).transpose(0, 1)), dict(lse=z(3, heads)),
+                   dict(lse=z(2, heads, dtype=torch.float32)), dict(table=z(1, 2, dtype=torch.int32, device="cpu")), dict(scale=1e-60)] + [b for b in bad if set(b) & {"k_pages", "v_pages", "table"}]:
+        with pytest.raises(ValueError):
+            attend.run_device(batch, **{**good, **change})
+    for scale in (-1.0, float("nan"), float("inf")):
+        with pytest.raises(binding.TtsError):
+            attend.run_device(batch, **good, scale=scale)
+    x = z(3, heads, d)
+    rotary.run_device(x, x)
+    for args in ((z(3, heads, d, device="cpu"), x), (x, z(2, heads, d)), (x, z(3, heads, d, dtype=torch.float32)), (z(3, heads, 40), x), (z(3, d, heads).transpose(1, 2), x)):
+        with pytest.raises(ValueError):
+            rotary.run_device(*args)
+    for more in (dict(positions=z(2, dtype=torch.int32)), dict(positions=z(3, dtype=torch.int64)), dict(positions=z(6, dtype=torch.int32)[::2]), dict(first=1 << 31)):
+        with pytest.raises(ValueError):
+            rotary.run_device(x, x, **more)
+    torch.cuda.synchronize()
+
+
+def test_streams_that_wait_for_each_other():
+    """Objects on streams of their own, tensors of the default one, and an event between them, as the headers ask: what is queued later on a stream sees what was ahead."""
+    import torch
+    heads, kv, d, page, n = 4, 2, 64, 16, 400
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    cache = binding.Cache(binding.make_cache_config(kv, d, page, binding.make_rotary_angles(d), n_heads=heads), stream=one)
+    attend = binding.PagedAttention(binding.make_paged_config(heads, kv, d, page), stream=two)
+    table = torch.arange(-(-n // page), dtype=torch.int32, device="cuda:0")[None]
+    kp, vp = (torch.zeros(table.shape[1], kv, page, d, device="cuda:0") for _ in range(2))
+    q_out, out = (torch.zeros(n, heads, d, device="cuda:0") for _ in range(2))
+    new, batch = cache.batch([n], [0], [0]), attend.batch([n], [n], [0])
+    want = None
+    for i in range(3):
+        g = torch.Generator(device="cuda:0").manual_seed(5)
+        k, v, q = (torch.randn(n, h, d, generator=g, device="cuda:0") for h in (kv, kv, heads))
+        one.wait_stream(torch.cuda.current_stream())
+        cache.run_device(new, k, v, kp, vp, table, q=q, q_out=q_out)
+        two.wait_stream(one)
+        attend.run_device(batch, q_out, kp, vp, table, out)
+        torch.cuda.current_stream().wait_stream(two)
+        got = out.clone()
+        for t in (kp, vp, q_out, out):
+            t.zero_()
+        torch.cuda.synchronize()
+        assert bool(torch.isfinite(got).all()) and float(got.abs().max()) > 0.1
+        want = got if want is None else want
+        assert torch.equal(got, want), i

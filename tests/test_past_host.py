@@ -271,6 +271,8 @@ def test_plans_of_attention(lib, heads, kv, d, bf16):
     ((8, 8, 64), [1] * 64, 300, [-1] * 64, [2000], dict(few=1, many=0, pools=0, joins=0)),               # nobody's prefix is not read
     ((4, 4, 64), [1], 9000, [-1], [], dict(few=1, many=0, pools=0, joins=1)),                            # a long sequence in parts
     ((16, 4, 128), [2000] * 8, 2000, [0] * 8, [500], dict(few=0, many=1, pools=0, joins=0)),             # many rows
+    ((32, 8, 128), [128], 4224, [-1], [], dict(few=0, many=1, pools=0, joins=1, split=1)),               # many rows of one request over parts of its keys
+    ((8, 2, 64), [40], 40, [-1], [], dict(few=1, many=0, pools=0, joins=0)),                             # many, but soon done
 ])
 def test_how_calls_are_taken(lib, shape, q_len, own, prefix, lens, want):
     lib.past_reset()
