@@ -800,6 +800,8 @@ template <int D, int NW, int R, bool FULL, typename Args> __global__ __launch_bo
 }
 
 // A row from its parts, its own keys' and its prefix's: their maxima give each a weight, then the row's waves take parts in turn, a column or two a lane, and meet in LDS.
+// Bound by latency: 4096 rows of 17 parts, 36 MB, take 12.0 us by a wave a row, eight parts a turn of the loop (four: 13.1; all eight asked for ahead of the first's use: 13.1); by four waves a row
+// 3 more, which fewer rows fill the card with.
 constexpr int JOIN_WAVES = 4;
 template <typename T, int D, int ACROSS, typename Args> __global__ __launch_bounds__(JOIN_WAVES * 64) void k_paged_join(Args p)
 {
@@ -844,7 +846,7 @@ template <typename T, int D, int ACROSS, typename Args> __global__ __launch_boun
     };
     float m = -__builtin_inff(), l = 0, o[PER] = {};
     if (todo) {
-#pragma unroll 4
+#pragma unroll 8
         for (int n = of_row; n < parts; n += ACROSS) {
             int height, in_tile;
             const float* part = part_at(n, height, in_tile);
