@@ -154,9 +154,13 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
     for (int i = 0; i < b->n; ++i) order[count[prefix_of(i) + 1]++] = i;
     auto rows_of = [&](int i) { return (long long)b->q_len[i] * group; };
     // small requests beside large ones are a launch with them, if that is a small one
-    bool mixed = false;
-    for (int i = 0; i < b->n; ++i) mixed |= rows_of(i) > 0 && rows_of(i) < PAGED_MANY_ROWS;
-    const bool any_many = bf16 && (!mixed || paged_many(few_tiles, p->n_cu));
+    bool small = false, large = false;
+    for (int i = 0; i < b->n; ++i) {
+        const long long rows = rows_of(i);
+        small |= rows > 0 && rows < PAGED_MANY_ROWS;
+        large |= rows >= PAGED_MANY_ROWS;
+    }
+    const bool any_many = bf16 && (!small || paged_many(few_tiles, p->n_cu)), any_whole = large && !any_many && few_tiles > 1024;
     auto form_of = [&](int i) {
         return any_many && rows_of(i) >= PAGED_MANY_ROWS ? Form::MANY : rows_of(i) < PAGED_MANY_ROWS || few_tiles <= 1024 ? Form::FEW : Form::WHOLE;
     };
@@ -164,6 +168,7 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
     HIP_TRY(on.err);
     const int room = paged_room(c.n_kv_heads);
     for (Form form : {Form::FEW, Form::WHOLE, Form::MANY}) {
+        if (form == Form::FEW ? !small && (any_many || any_whole) : form == Form::WHOLE ? !any_whole : !any_many || !large) continue;
         auto tiles_of = [&](long long rows) { return (rows + 15) / 16 * c.n_kv_heads; };
         long long tiles = 0;                 // of the requests and of the prefixes before the last one, which need room for a part each
         int last_prefix = -1;
@@ -182,7 +187,7 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
             a.q_first = a.req[0].q_row;
             for (int i = 1; i < a.n; ++i) {
                 if (a.row[i + 1] - a.row[i] != a.row[1]) a.each = 0;
-                if (a.req[i].q_row != a.req[0].q_row + a.row[i] / group) a.q_first = -1;
+                if ((a.req[i].q_row - a.req[i - 1].q_row) * group != a.row[i] - a.row[i - 1]) a.q_first = -1;
             }
             hipError_t e;
             // what the cheapest way should take: prefixes ahead of each request's own rows, as tiles of their own beside them, or as a launch of larger ones; larger tiles for requests, too
@@ -198,9 +203,11 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
                 const PagedCut beside = paged_cut(a, PagedPools::TILES, bytes, p->n_cu, unique, room);
                 if (beside.ns < cut.ns) cut = beside;
                 height = bf16 ? paged_pool_height(a, p->n_cu) : 0;
+                const double pools_ns = height ? paged_pools_ns(a, height, p->n_cu) : 0;
+                if (height && pools_ns >= cut.ns) height = 0;
                 if (height) {
                     PagedCut apart = paged_cut(a, PagedPools::APART, bytes, p->n_cu, unique, 8 * p->n_cu);
-                    apart.ns += paged_pools_ns(a, height, p->n_cu);
+                    apart.ns += pools_ns;
                     if (apart.ns < cut.ns) cut = apart;
                     else height = 0;
                 }
@@ -214,6 +221,7 @@ extern "C" int tts_paged_run(tts_paged* p, const tts_paged_batch* b, const tts_p
                 plan_paged_many(a, cut);
                 e = launch_paged_many(a, PAGED_MANY_HEIGHT, p->stream);
             } else {
+                even_parts(a, cut);
                 plan_paged_few(a, cut);
                 e = launch_paged_few(a, bf16, p->n_cu, p->stream);
                 if (e == hipSuccess && height) {

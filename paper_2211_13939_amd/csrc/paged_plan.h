@@ -78,7 +78,7 @@ inline PagedCut paged_cut(const PagedArgs& a, PagedPools pools, int element_byte
     while (whole < longest) whole *= 2;
     for (int log = log2_of(whole); log >= 6; --log) {
         long long items = 0;
-        for (int i = 0; i < t.n; ++i) items += (long long)t.tiles[i] * std::max(1, (t.len[i] + (1 << log) - 1) >> log);
+        for (int i = 0; i < t.n; ++i) items += (long long)t.tiles[i] * (((std::max(t.len[i], 1) - 1) >> log) + 1);
         const int parts = std::max(1, (longest + (1 << log) - 1) >> log);
         const bool eight = items <= n_cu;
         if ((parts > 1 || pools != PagedPools::NONE) && items > room) break;
@@ -95,16 +95,23 @@ inline PagedCut paged_cut(const PagedArgs& a, PagedPools pools, int element_byte
         if (ns < best.ns) best = PagedCut{pools, parts > 1 ? 1 << log : 0, ns};
         if (items > 2 * at_once && parts > 1) break;
     }
-    if (best.share) {                    // the longest sequence's parts of one length, where that makes no more of them for others
-        const int parts = (longest - 1) / best.share + 1, even = ((longest + parts - 1) / parts + 31) / 32 * 32;
-        long long items = 0, evenly = 0;
-        for (int i = 0; i < t.n; ++i) {
-            items += (long long)t.tiles[i] * paged_parts(t.len[i], best.share);
-            evenly += (long long)t.tiles[i] * paged_parts(t.len[i], even);
-        }
-        if (evenly <= items) best.share = even;
-    }
     return best;
+}
+// The longest sequence's parts of one length, where that makes no more of them for others.
+inline void even_parts(const PagedArgs& a, PagedCut& cut)
+{
+    if (!cut.share) return;
+    const PagedTiles t = paged_tiles(a, cut.pools);
+    int longest = 0;
+    for (int i = 0; i < t.n; ++i) longest = std::max(longest, t.len[i]);
+    const int parts = (longest - 1) / cut.share + 1, even = ((longest + parts - 1) / parts + 31) / 32 * 32;
+    if (even == cut.share) return;
+    long long items = 0, evenly = 0;
+    for (int i = 0; i < t.n; ++i) {
+        items += (long long)t.tiles[i] * paged_parts(t.len[i], cut.share);
+        evenly += (long long)t.tiles[i] * paged_parts(t.len[i], even);
+    }
+    if (evenly <= items) cut.share = even;
 }
 
 // Numbers of a launch's tiles; pools: of prefixes of their own in it.
