@@ -193,12 +193,13 @@ inline int paged_pool_height(const PagedArgs& a, int n_cu)
     for (int i = 0; i < a.n; ++i) own += (a.row[i + 1] - a.row[i] + 15) / 16 * a.n_kv_heads;
     return tiles * height <= (paged_room(a.n_kv_heads) - std::max<long long>(own, 8 * n_cu)) * PAGED_FEW_ROWS ? height : 0;
 }
-// What they should take, with the kernel that joins their rows (us: a tile's 64 keys 1.9 with a workgroup a compute unit, 3 with two).
+// What they should take, with the kernel that joins their rows: a tile's 64 keys 1.2 us of a compute unit (0.85 with heads of 64), its part's way out with them (512 rows of 8 heads over
+// 16001 keys, in 16 parts, 48 us), then some ten parts of every row.
 inline double paged_pools_ns(const PagedArgs& a, int height, int n_cu)
 {
     double work = 0;
-    for (int g = 0; g < a.n_pools; ++g) work += (double)((pool_rows(a, g) + height - 1) / height) * a.n_kv_heads * (a.pool[g].len / 64 + 1) * 1500;
-    return 9000 + work / n_cu + 5000 + (double)a.rows * a.n_kv_heads * 10 * 520 / 3500;
+    for (int g = 0; g < a.n_pools; ++g) work += (double)((pool_rows(a, g) + height - 1) / height) * a.n_kv_heads * (a.pool[g].len / 64 + 1);
+    return 9000 + work * (a.head_dim > 64 ? 1200 : 850) / n_cu + 5000 + (double)a.rows * a.n_kv_heads * 10 * 520 / 3500;
 }
 inline void plan_paged_pools(PagedArgs& a, int height, int n_cu)
 {
