@@ -342,12 +342,12 @@ template <typename T, int D, bool FULL> struct PagedRunning : Operands<T, D> {
 #pragma unroll
         for (int e = 0; e < G::NE; ++e) o[e] *= by;
     }
-    // Keys that there are not: no value either (0 times an infinity would be NaN); of those from `clear` on, which not all rows see, no infinities and NaN.
+    // Keys that there are not, or not for any row (from `end` on): no value either (0 times an infinity would be NaN); of those from `clear` on, which not all rows see, no infinities and NaN.
     __device__ __forceinline__ void mend(const int (&n)[G::TILES], int first, int clear, int end, int g)
     {
 #pragma unroll
         for (int i = 0; i < G::PER_LANE; ++i) {
-            const uint32_t there = 4 * g + (i & 3) < n[i / 4] ? ~0u : 0u;
+            const uint32_t there = 4 * g + (i & 3) < min(n[i / 4], end - first - 16 * (i / 4)) ? ~0u : 0u;
 #pragma unroll
             for (int e = 0; e < WORDS; ++e) v[i][e] &= there;
         }
