@@ -93,7 +93,7 @@ template <int N> __device__ __forceinline__ void arrived()
     static_assert(N < 64, "the counter has six bits");
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
-// (written out as in linear8.hip: no registers to come back to)
+// (written out, as in lds_loads.h; addresses are the lanes')
 __device__ __forceinline__ void to_lds(const char* from, uint32_t to)
 {
     uint32_t m0;

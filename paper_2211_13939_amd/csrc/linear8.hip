@@ -6,6 +6,7 @@
 // the t-th of two units is channel 32 h + 16 t + 4 a + j of the 64: a lane of that instruction has 16 neighbouring channels of a unit.
 #include "operator_kernels.h"
 #include "mfma.h"
+#include "lds_loads.h"
 
 namespace tts {
 
@@ -133,17 +134,7 @@ template <typename YT> __global__ __launch_bounds__(FEW_WAVES * 64) void k_linea
 // lanes bring the 64 bytes of a row (lanes of rows apart, as the operand has them, take a cycle of the load path each: 128 x 128 tiles of
 // 16384 x 4096 x 4096 353 in place of 305 us), each the quarter that its place is for: rows' quarters change places every four rows, so that the
 // operand's reads of 16 bytes find all banks.
-//
-// These loads are written out: of the builtin the compiler does not know which of two buffers it fills, and waits for it in front of every read of the
-// other.  They have no registers to come back to; what they bring is there behind arrived().  m0, where it goes, is
-// theirs: they set it themselves, and its old value is no longer there.
-template <int BYTES> __device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t offset, uint32_t to)
-{
-    static_assert(BYTES == 16 || BYTES == 4, "");
-    uint32_t m0;
-    if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" : "={m0}"(m0) : "s"(to), "v"(offset), "s"(base) : "memory");
-    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, %3" : "={m0}"(m0) : "s"(to), "v"(offset), "s"(base) : "memory");
-}
+
 // All but the last N loads of every wave are there, and all waves have read what they needed.
 template <int N> __device__ __forceinline__ void arrived()
 {
@@ -232,19 +223,19 @@ template <typename YT, int TN, int TM, int WN, int WM, int SUB, int STEPS> struc
 #pragma unroll
         for (int i = 0; i < W_LOADS; ++i) {
             const int c = wave + i * WAVES;
-            to_lds<16>(w_at[i] + (size_t)step * (2048 * SUB), lane * 16, to + c / (2 * NT) * PART + c % (2 * NT) * 1024);
+            to_lds_from<16>(w_at[i] + (size_t)step * (2048 * SUB), lane * 16, to + c / (2 * NT) * PART + c % (2 * NT) * 1024);
         }
 #pragma unroll
         for (int i = 0; i < X_LOADS; ++i) {
             const int c = wave + i * WAVES;
-            to_lds<16>(x_at + (size_t)step * (64 * SUB), x_off[i], to + c / (2 * MT) * PART + NT * 2048 + c % (2 * MT) * 1024);
+            to_lds_from<16>(x_at + (size_t)step * (64 * SUB), x_off[i], to + c / (2 * MT) * PART + NT * 2048 + c % (2 * MT) * 1024);
         }
     }
     __device__ __forceinline__ void bring_scales(int word) const
     {
 #pragma unroll
         for (int i = 0; i < S_LOADS; ++i)
-            if (2 * (wave + i * WAVES) < NT + MT) to_lds<4>(s_base[i] + (size_t)word * s_step[i], s_off[i], lds_at + STEPS * STEP + (word & 1) * SCALES + (wave + i * WAVES) * 256);
+            if (2 * (wave + i * WAVES) < NT + MT) to_lds_from<4>(s_base[i] + (size_t)word * s_step[i], s_off[i], lds_at + STEPS * STEP + (word & 1) * SCALES + (wave + i * WAVES) * 256);
     }
     __device__ __forceinline__ Frag8 w_frag(int part, int unit) const
     {
@@ -389,10 +380,10 @@ template <typename YT> __global__ __launch_bounds__(SPLIT_WAVES * 64, 2) void k_
     auto bring = [&](int turn) {
         const uint32_t to = ring_at + turn % SPLIT_RING * SPLIT_SLOT;
         const size_t step = (size_t)turn * SPLIT_WAVES + wave;
-        to_lds<16>(w_at + step * 2048, lane * 16, to);
-        to_lds<16>(w_at + step * 2048 + 1024, lane * 16, to + 1024);
+        to_lds_from<16>(w_at + step * 2048, lane * 16, to);
+        to_lds_from<16>(w_at + step * 2048 + 1024, lane * 16, to + 1024);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) to_lds<16>(x_at + step * 64, x_off[c], to + 2048 + c * 1024);
+        for (int c = 0; c < 2; ++c) to_lds_from<16>(x_at + step * 64, x_off[c], to + 2048 + c * 1024);
         lane_to_lds(s_at + turn * s_step, to + 4096);
     };
     floatx16 acc[1] = {};

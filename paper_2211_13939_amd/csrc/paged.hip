@@ -5,6 +5,7 @@
 // Keys come 16 at a time: pages have whole 16s, so that 16 keys of a head lie back to back in one page, whose number is the wave's, not the lane's, to look up.
 #include "past_kernels.h"
 #include "attend.h"
+#include "lds_loads.h"
 #include "words.h"
 
 #include <algorithm>
@@ -634,12 +635,6 @@ template <int D, int NW, int R> struct PagedMany {
     static constexpr int LDS = R * SLOT + SIXTEENS * 10 + 16;            // 8 bytes for where 16 keys lie, 2 for which of them there are; whether a value was taken out
     static_assert(LOADS * 1024 * NW == PART, "shares of the waves");
 };
-// 16 bytes a lane to LDS, from a wave's address and a lane's offset
-__device__ __forceinline__ void to_lds_from(const char* base, uint32_t offset, uint32_t to)
-{
-    uint32_t m0;
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" : "={m0}"(m0) : "s"(to), "v"(offset), "s"(base) : "memory");
-}
 
 template <int D, int NW, int R, bool FULL, typename Args> __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 3) void k_paged_many(Args p)
 {
@@ -710,8 +705,8 @@ template <int D, int NW, int R, bool FULL, typename Args> __global__ __launch_bo
 #pragma unroll
         for (int i = 0; i < M::LOADS; ++i) {
             const uint32_t to = lds_at + slot * M::SLOT + (wave + i * NW) * 1024;
-            if (k_there[i]) to_lds_from(kp + from[i], k_offset[i], to);
-            if (v_there[i]) to_lds_from(vp + from[i], v_offset[i], to + M::PART);
+            if (k_there[i]) to_lds_from<16>(kp + from[i], k_offset[i], to);
+            if (v_there[i]) to_lds_from<16>(vp + from[i], v_offset[i], to + M::PART);
         }
     };
     if (!FULL)                           // (columns that there are not: zeros, which nothing is loaded over)
