@@ -628,8 +628,10 @@ template <typename T, int D, bool FULL, int WAVES, typename Args> __global__ __l
 // Bound by the matrix pipe's and the softmax's turns, one behind the other in a wave: a tile's 64 keys take a workgroup of 128 rows by itself 1.25 us (columns 128; 64: 0.9), two of them a
 // compute unit 0.97 each (three of 64: 0.69), 1.1 PFLOP/s of the pipe's 2.5 (8 prompts of 1500 to 4000 behind a prefix of 500, 16 heads of 128 that share 4: 478 us, 0.88 over the scores
 // that count). A second workgroup a compute unit is worth more than taller tiles (2 slots of 32 KB and 232 registers leave room for it): 256 rows, three slots, took 289 us for 2 requests of
-// 4096 where 128 take 294, but 72 against 56 for one of 512 over 2560. All waves take all of the workgroup's tiles: skipping those that a wave's rows do not see made the compiler keep every
-// sum twice (copies and spilled registers: the prompts 588 us, and copies that now and then came too early where two workgroups shared a compute unit).
+// 4096 where 128 take 294, but 72 against 56 for one of 512 over 2560. All waves take all of the workgroup's tiles: where they skipped
+// those that their rows do not see, the compiler kept every sum twice and copied all of them each tile, with registers in scratch memory besides (the prompts 588 us).  Two such forms gave wrong results
+// now and then with two workgroups a compute unit, and why is not known: by its code the copies stood as far behind the matrix instructions as they have to (48 more cycles there changed nothing), no scalar
+// register was read too early, and barriers and waits are the ones below.  The build ends if this kernel spills again.
 template <int D, int NW, int R> struct PagedMany {
     static constexpr int ROW = 2 * D, PART = KEYS * ROW, SLOT = 2 * PART, LOADS = PART / 1024 / NW, AHEAD = 64, SIXTEENS = 2 * AHEAD * KEYS / 16;
     static constexpr int LDS = R * SLOT + SIXTEENS * 10 + 16;            // 8 bytes for where 16 keys lie, 2 for which of them there are; whether a value was taken out
@@ -749,7 +751,7 @@ template <int D, int NW, int R, bool FULL, typename Args> __global__ __launch_bo
             if (bad) *odd = 1;
             lds_barrier();
         }
-        // (by all waves, also those whose rows end before: the tile's barrier waits for the others, and a branch here has the compiler copy all sums from turn to turn)
+        // (by all waves, also those whose rows end before: the tile's barrier waits for the others, and a branch here had the compiler copy all sums from turn to turn)
         const int seen = min(limit, end) - key;
         const uint64_t own = key + KEYS <= clear ? mask : mask & (seen >= KEYS ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
         run.template take<2>(keys, values, mask != ~0ull || key + KEYS > clear, own, p.scale, lane);
