@@ -630,7 +630,7 @@ template <typename T, int D, bool FULL, int WAVES, typename Args> __global__ __l
 // that count). A second workgroup a compute unit is worth more than taller tiles (2 slots of 32 KB and 232 registers leave room for it): 256 rows, three slots, took 289 us for 2 requests of
 // 4096 where 128 take 294, but 72 against 56 for one of 512 over 2560. All waves take all of the workgroup's tiles: where they skipped
 // those that their rows do not see, the compiler kept every sum twice and copied all of them each tile, with registers in scratch memory besides (the prompts 588 us).  Two such forms gave wrong results
-// now and then with two workgroups a compute unit, and why is not known: by its code the copies stood as far behind the matrix instructions as they have to (48 more cycles there changed nothing), no scalar
+// now and then with two workgroups a compute unit, and why is not known: by its code the copies stood as far behind the matrix instructions as they have to (48 more wait states there changed nothing), no scalar
 // register was read too early, and barriers and waits are the ones below.  The build ends if this kernel spills again.
 template <int D, int NW, int R> struct PagedMany {
     static constexpr int ROW = 2 * D, PART = KEYS * ROW, SLOT = 2 * PART, LOADS = PART / 1024 / NW, AHEAD = 64, SIXTEENS = 2 * AHEAD * KEYS / 16;
