@@ -41,11 +41,34 @@ PREFIX = {
     "prefix_64_of_128": _steps(32, 8, 128, 64, 32, [16000, 15993]), "prefix_64_of_64": _steps(32, 16, 64, 16, 128, [16000, 15993, 15986, 15979]),
     "prefix_64_of_96": _steps(16, 8, 96, 16, 128, [16000, 15993, 15986, 15979]), "prefix_64_of_40": _steps(32, 32, 40, 32, 64, [32000]),
 }
-CASES = {**MANY, **PARTS, **PREFIX}
+
+
+def _chunks(heads, kv, d, page, n, q, lens, bf16=True):
+    """Chunks of many requests, some of them half as long, most behind a prefix."""
+    q_len = [q if i % 5 else q // 2 for i in range(n)]
+    return dict(heads=heads, kv=kv, d=d, page=page, bf16=bf16, causal=True, q_len=q_len, own_len=[a + (53 * i) % 300 for i, a in enumerate(q_len)],
+                prefix=[i % len(lens) if i % 5 != 4 else -1 for i in range(n)], prefix_len=lens)
+
+
+# Requests of both kinds in one call, and of many rows that tiles of 16 take, in fp32 always: with the plan of each
+CHUNKS = {
+    "chunks_64": (_chunks(8, 8, 64, 16, 32, 40, [700, 1500]), dict(few=2, many=0, joins=2, pools=4, split=5, height=0)),
+    "chunks_64_long": (_chunks(8, 8, 64, 64, 32, 40, [4000, 3993]), dict(few=2, many=1, joins=2, pools=4, split=4, height=128)),
+    "chunks_128_long": (_chunks(16, 4, 128, 64, 32, 40, [16000, 15993]), dict(few=1, many=1, joins=1, pools=2, split=2, height=128)),
+    "chunks_40_long": (_chunks(16, 8, 40, 32, 32, 40, [16000, 15993]), dict(few=1, many=1, joins=1, pools=2, split=2, height=128)),
+    "chunks_40_ahead": (_chunks(16, 8, 40, 16, 32, 40, [700, 1500]), dict(few=1, many=0, joins=0, pools=0, split=0, height=0)),
+    "chunks_40_fp32": (_chunks(16, 8, 40, 32, 64, 20, [4000, 3993], False), dict(few=2, many=0, joins=1, pools=2, split=2, height=0)),
+    "chunks_128_fp32": (_chunks(16, 4, 128, 64, 24, 150, [500, 400], False), dict(few=1, many=0, joins=0, pools=0, split=0, height=0)),
+    "chunks_128_fp32_long": (_chunks(16, 4, 128, 64, 32, 40, [16000, 15993], False), dict(few=1, many=0, joins=1, pools=0, split=26, height=0)),
+    "chunks_64_fp32": (_chunks(8, 8, 64, 16, 24, 150, [4000], False), dict(few=1, many=0, joins=0, pools=0, split=0, height=0)),
+}
+CASES = {**MANY, **PARTS, **PREFIX, **{name: case for name, (case, _) in CHUNKS.items()}}
 
 
 def plan(name):
     """Launches of few and of many rows, of what joins parts, prefixes read apart, and the height of the tiles of many rows."""
+    if name in CHUNKS:
+        return CHUNKS[name][1]
     if name in MANY:
         return dict(few=0, many=1, joins=0, pools=0, split=0, height=128)
     if name in PARTS:

@@ -1,5 +1,5 @@
-"""tts_paged in each way that a call can be taken by the kernel of many rows (paged_cases.py; that the calls are taken so is held by test_paged_forms_host.py): whole requests, parts of their keys, prefixes
-in tiles of 64 and 128; heads of every width, pages that there are not, what is not seen and what it holds, values that are no numbers, strides, addresses past 32 bits, graphs."""
+"""tts_paged in each way that a call of many rows, or over long prefixes, can be taken (paged_cases.py; that the calls are taken so is held by test_paged_forms_host.py): whole requests, parts of their keys,
+prefixes in tiles of 64 and 128, requests of both kinds in one call; heads of every width, pages that there are not, what is not seen and what it holds, values that are no numbers, strides, addresses past 32 bits, graphs."""
 import numpy as np
 import pytest
 
@@ -16,7 +16,7 @@ def _case(name, **more):
     import torch
     c = CASES[name]
     say(f"case paged form {name} {more if 'gone' not in more else 'pages gone'}")
-    return Case(torch, c["heads"], c["kv"], c["d"], c["page"], True, c["q_len"], c["own_len"], c["prefix"], c["prefix_len"], causal=c["causal"], **{"seed": len(name), **more})
+    return Case(torch, c["heads"], c["kv"], c["d"], c["page"], c.get("bf16", True), c["q_len"], c["own_len"], c["prefix"], c["prefix_len"], causal=c["causal"], **{"seed": len(name), **more})
 
 
 def _want(c):
@@ -25,7 +25,7 @@ def _want(c):
 
 def _check_rows(c, out, lse, want, rows):
     at = c.torch.from_numpy(np.flatnonzero(rows)).to("cuda:0")
-    _check(out[at], lse[at], [w[rows] for w in want], c.shape[2], c.longest, True)
+    _check(out[at], lse[at], [w[rows] for w in want], c.shape[2], c.longest, c.bf16)
 
 
 @pytest.mark.parametrize("name", CASES)
@@ -34,7 +34,7 @@ def test_form(name):
     want = _want(c)
     c.check(want=want)
     out, _ = c.run(lse=False)
-    _check(out, None, want, c.shape[2], c.longest, True)
+    _check(out, None, want, c.shape[2], c.longest, c.bf16)
 
 
 def _gone(name):
@@ -50,7 +50,8 @@ def _gone(name):
 
 
 @pytest.mark.parametrize("name", ["many_64", "many_40", "many_72", "many_128", "many_64_all", "parts_128", "parts_64", "parts_40", "parts_128_own", "parts_64_own", "parts_128_short", "parts_64_short",
-                                  "parts_64_all", "prefix_128_of_128", "prefix_128_of_40", "prefix_64_of_128", "prefix_64_of_40"])
+                                  "parts_64_all", "prefix_128_of_128", "prefix_128_of_40", "prefix_64_of_128", "prefix_64_of_40", "chunks_64", "chunks_64_long", "chunks_40_fp32", "chunks_128_fp32",
+                                  "chunks_128_fp32_long"])
 def test_what_is_not_seen_holds_anything(name):
     """Rows behind a sequence's last, pages of nobody, pages that are gone and, for a query, the rows behind its own: infinities and NaN there are not used."""
     c = _case(name, gone=_gone(name))
@@ -92,7 +93,7 @@ def test_what_is_not_seen_holds_anything(name):
     c.check(want=want)
 
 
-@pytest.mark.parametrize("name", ["many_64", "many_40", "many_128", "many_64_all", "parts_64", "parts_128_own", "prefix_128_of_128"])
+@pytest.mark.parametrize("name", ["many_64", "many_40", "many_128", "many_64_all", "parts_64", "parts_128_own", "prefix_128_of_128", "chunks_64", "chunks_128_fp32"])
 def test_values_that_are_no_numbers_for_those_that_see_them(name):
     """An infinity that a query sees is its result's, with its sign; two of both signs, or a NaN, make NaN."""
     c = _case(name)
@@ -126,7 +127,7 @@ def test_strides_and_a_scale(name):
     c.check(want=_want(c))
 
 
-@pytest.mark.parametrize("name", ["many_64", "many_128", "parts_64", "parts_128_own", "prefix_128_of_128", "prefix_64_of_128"])
+@pytest.mark.parametrize("name", ["many_64", "many_128", "parts_64", "parts_128_own", "prefix_128_of_128", "prefix_64_of_128", "chunks_64_long", "chunks_40_fp32"])
 def test_loud_scores(name):
     """Scores of hundreds: the running maximum carries them, across parts too; one key takes all."""
     c = _case(name, size=12)
@@ -165,7 +166,7 @@ def test_a_graph_on_a_stream_of_its_own(name):
         op.run_device(half, c.q[:1], c.k, c.v, c.table, outs[1][:1])
     rng, before, pages = np.random.default_rng(1), None, -(-own[0] // page)
     for i in range(4):
-        c.q.copy_(_rows(torch, rng, c.q.shape[0], c.shape[0], c.shape[2], True))
+        c.q.copy_(_rows(torch, rng, c.q.shape[0], c.shape[0], c.shape[2], c.bf16))
         c.table[0, :pages] = c.table[0, :pages].flip(0).clone()
         torch.cuda.synchronize()
         with torch.cuda.stream(op.stream):

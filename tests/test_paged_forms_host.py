@@ -12,7 +12,7 @@ from tests.test_past_host import _paged, lib  # noqa: F401
 @pytest.mark.parametrize("name", CASES)
 def test_how_the_cases_are_taken(lib, name):  # noqa: F811
     c, want = CASES[name], plan(name)
-    m = Made(lib, "paged", binding.make_paged_config(c["heads"], c["kv"], c["d"], c["page"], True, c["causal"]))
+    m = Made(lib, "paged", binding.make_paged_config(c["heads"], c["kv"], c["d"], c["page"], c.get("bf16", True), c["causal"]))
     lib.past_reset()
     assert _paged(lib, m, c["q_len"], c["own_len"], [0] * len(c["q_len"]), c["prefix"], c["prefix_len"], [1] * len(c["prefix_len"]), table_cols=3000) == 0
     assert {k: getattr(lib, f"past_{k}")() for k in want} == want
